@@ -37,8 +37,11 @@ STAGES = {
     "attn_fwd": ("k_fwd_mfma", "k_fwd_f32", "k_fwd_genericT"),
     "attn_bwd": ("k_bwd_dq", "k_bwd_dkv", "k_bwd_dkv_reduce", "k_bwd_dq_f32", "k_bwd_dkv_f32", "k_bwd_dkv_f32_sum", "k_bwd_dq_genericT",
                  "k_bwd_dkv_genericT", "k_bwd_scatter_dkv", "k_bwd_acc_finish", "k_compact_kv"),   # k_compact_kv runs in both calls
-    "decode_attn": ("k_decode_mfma", "k_decode_attn", "k_decode_combine"),
+    "decode_attn": ("k_decode_mfma", "k_decode_attn", "k_decode_combine", "k_decode_combine_acc"),
     "cache_compress": ("k_cache_compress", "k_cache_select_move", "k_cache_gather", "k_cache_place"),
+    "cache_evict": ("k_evict_select", "k_evict_rows", "k_evict_quant"),
+    "cache_quant": ("k_append_quant", "k_read_quant"),
+    "decode_attn_quant": ("k_decode_quant", "k_quant_combine"),
 }
 
 

@@ -274,6 +274,95 @@ int lrsa_decode_attn(const lrsa_params *p, const void *q, const void *Kc, const 
 int lrsa_decode_attn_static(const lrsa_params *p, const void *q, const void *Kc, const void *Vc, int32_t len,
                             void *O, float *lse, void *stream);
 
+/* ---- eviction by accumulated attention weight: instead of a score of the rows themselves (Eq. 4-8), the weight that a row
+ * has received from the tokens so far decides whether it stays.
+ *
+ * lrsa_decode_attn_acc: lrsa_decode_attn that also adds up those weights.  With w[g, r] the softmax weight of row r for query
+ * head g of a KV group, for every (batch, KV head) and rows r < len:
+ *   acc_out[r] = decay * acc_in[r] + sum over the G heads of w[g, r]
+ *   acc_in  : [B, Hkv, cap] fp32, contiguous, or NULL: zeros                     (device, read)
+ *   acc_out : [B, Hkv, cap] fp32, contiguous; rows at and behind len are left as they were; may be acc_in
+ *                                                                                (device, written)
+ *   decay   : finite; 1 adds up, less than 1 forgets
+ * The other arguments are those of lrsa_decode_attn, O and lse its results bit for bit.
+ * Workspace: lrsa_decode_attn_acc_ws_bytes(p, len), which is larger for larger len. */
+size_t lrsa_decode_attn_acc_ws_bytes(const lrsa_params *p, int32_t len);
+int lrsa_decode_attn_acc(const lrsa_params *p, const void *q, const void *Kc, const void *Vc, int32_t len, const float *acc_in,
+                         float *acc_out, float decay, void *O, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* lrsa_cache_evict: of a cache with more than `budget` rows, the first `sink` (of the params), the last `recent` and the
+ * budget - sink - recent rows between them with the largest acc stay (equal ones: the lowest first), per (batch, KV head), in
+ * position order; a cache with fewer keeps all.  They go to ANOTHER cache of the same layout, which a program swaps with the
+ * old one (one spare for all layers is enough); the old one is left as it was.
+ *   Kc, Vc, Ko, Vo : [B, Hkv, cap, d_h] by kv_stride; cap = p->seq; Ko, Vo rows behind the new length are left as they were
+ *   pos, pos_o     : [B, Hkv, cap] int32, contiguous, moved alike; both may be NULL
+ *   acc            : [B, Hkv, cap] fp32, contiguous, any finite values             (device, read)
+ *   acc_o          : like acc: the weights of the rows that stay, and ZERO in all rows behind them, so that rows appended
+ *                    later begin with none                                         (device, written)
+ *   len, budget, recent : host values; 0 <= len <= cap, sink + recent <= budget <= cap, budget >= 1, recent >= 0
+ *   len_out        : HOST pointer, receives min(len, budget)
+ * None of the outputs may overlap an input.  Workspace: lrsa_cache_evict_ws_bytes(p, len, budget). */
+size_t lrsa_cache_evict_ws_bytes(const lrsa_params *p, int32_t len, int32_t budget);
+int lrsa_cache_evict(const lrsa_params *p, const void *Kc, const void *Vc, const int32_t *pos, const float *acc, int32_t len,
+                     int32_t budget, int32_t recent, void *Ko, void *Vo, int32_t *pos_o, float *acc_o, int32_t *len_out,
+                     void *ws, size_t ws_bytes, void *stream);
+
+/* ---- the inference-time cache in 8 bits, with a scale for every block of rows and KV head.
+ *
+ * A row's value is code * scale of its block.  The scale is a power of two: the least 2^e, e >= -120, by which the block's
+ * largest magnitude does not exceed the largest code (int8: 127, e4m3: 448); the code is the nearest one to value / scale, ties
+ * to even.  Values are then exact in bf16, and rows that change their block keep their value unless the new block's scale is
+ * too coarse for it.  (The attention call takes any finite scales and int8 codes down to -128.)
+ *
+ * In these calls p->seq is cap, the rows that the cache has room for; dtype is that of q, O and of the rows K, V given to
+ * lrsa_cache_append_quant and taken by lrsa_cache_read_quant, which kv_stride describes; q_stride is not used.  Every sequence
+ * has a length of its own in DEVICE memory, lens [B] int32, so that a captured graph can be replayed while they grow; lengths
+ * below 0 count as 0 and lengths above the bound that a call names (max_len, else cap) as that bound. */
+typedef enum { LRSA_QUANT_INT8 = 0, LRSA_QUANT_E4M3 = 1 /* OCP e4m3: no infinities */ } lrsa_quant_format;
+typedef struct {
+    int32_t format;        /* lrsa_quant_format                                                                       */
+    int32_t block;         /* rows per scale: 16, 32, 64 or 128                                                       */
+    int64_t stride[3];     /* BYTE strides of (batch, head, row) of K and V: row >= head_dim, all multiples of 16     */
+    void *K, *V;           /* codes [B, Hkv, cap, d_h] by stride, 16-byte aligned                                     */
+    float *K_scale, *V_scale; /* [B, Hkv, ceil(cap / block)] contiguous                                               */
+} lrsa_quant_cache;
+
+/* Rows lens[b] .. lens[b] + counts[b] - 1 of sequence b become the first counts[b] rows of K and V.  Where the first of them
+ * falls into a block with older rows, that block's scale grows if it must and its older codes are rounded to the new scale.  Rows
+ * that would lie at or behind cap are dropped; lens is not changed; codes behind the new rows are left as they were.
+ *   K, V   : [B, Hkv, tokens, d_h] by kv_stride, dtype `dtype`                     (device, read)
+ *   counts : [B] int32, 0 <= counts[b] <= tokens (others count as the nearer bound), or NULL: tokens of every sequence */
+int lrsa_cache_append_quant(const lrsa_params *p, const lrsa_quant_cache *c, const void *K, const void *V, int32_t tokens,
+                            const int32_t *lens, const int32_t *counts, void *stream);
+
+/* Rows first[b] .. first[b] + rows - 1 of sequence b as values; rows before 0 and at or behind lens[b] are zero.
+ *   first : [B] int32 or NULL: 0
+ *   K, V  : [B, Hkv, rows, d_h] by kv_stride, dtype `dtype`                        (device, written) */
+int lrsa_cache_read_quant(const lrsa_params *p, const lrsa_quant_cache *c, const int32_t *lens, int32_t rows, const int32_t *first,
+                          void *K, void *V, void *stream);
+
+/* Attention of the last `tokens` tokens of every sequence over the cache, whose last rows are theirs: token t sees the rows
+ * below lens[b] - tokens + 1 + t.  A token that sees none (a sequence shorter than `tokens`, padding) gets O = 0 and
+ * lse = -inf.
+ *   q   : [B, Hq, tokens, d_h] contiguous, dtype `dtype`, 1 <= tokens <= 16         (device, read)
+ *   O   : like q                                                                    (device, written)
+ *   lse : [B, Hq, tokens] fp32, may be NULL                                         (device, written)
+ *   max_len : 1 <= max_len <= cap, a bound of lens by which the work is divided
+ *   acc_in, acc_out, decay : as in lrsa_decode_attn_acc, the sum taken over the group's heads and the tokens; acc_out NULL (then
+ *         acc_in must be, too): no weights are added up
+ * Workspace: lrsa_decode_attn_quant_ws_bytes(p, tokens, max_len, acc_out != NULL). */
+size_t lrsa_decode_attn_quant_ws_bytes(const lrsa_params *p, int32_t tokens, int32_t max_len, int with_acc);
+int lrsa_decode_attn_quant(const lrsa_params *p, const lrsa_quant_cache *c, const void *q, int32_t tokens, const int32_t *lens,
+                           int32_t max_len, const float *acc_in, float *acc_out, float decay, void *O, float *lse, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* lrsa_cache_evict for a cache in 8 bits: from cache `c` to cache `o` (same format, block and cap, strides of its own), with the
+ * sequences' lengths lens -> lens_o [B] int32 (device; lens_o must not be lens).  A block of the new cache gets the scale of the
+ * rows that it now holds.  Workspace: lrsa_cache_evict_ws_bytes(p, max_len, budget). */
+int lrsa_cache_evict_quant(const lrsa_params *p, const lrsa_quant_cache *c, const int32_t *pos, const float *acc, const int32_t *lens,
+                           int32_t max_len, int32_t budget, int32_t recent, const lrsa_quant_cache *o, int32_t *pos_o, float *acc_o,
+                           int32_t *lens_o, void *ws, size_t ws_bytes, void *stream);
+
 /* Message of the calling thread's last failed call (static thread-local storage, never NULL). */
 const char *lrsa_last_error(void);
 

@@ -23,6 +23,8 @@ EXPORTS = ("lrsa_abi_version", "lrsa_last_error", "lrsa_num_scored_chunks", "lrs
            "lrsa_score", "lrsa_select", "lrsa_score_select", "lrsa_check_idx", "lrsa_attn_fwd", "lrsa_attn_bwd",
            "lrsa_cache_compress", "lrsa_cache_compress_ws", "lrsa_cache_compress_ws_bytes", "lrsa_decode_attn", "lrsa_decode_attn_static",
            "lrsa_fill_workspace_bytes", "lrsa_attn_bwd_parts", "lrsa_attn_plan", "lrsa_attn_fwd_fill", "lrsa_attn_bwd_fill", "lrsa_attn_bwd_finish",
+           "lrsa_decode_attn_acc", "lrsa_decode_attn_acc_ws_bytes", "lrsa_cache_evict", "lrsa_cache_evict_ws_bytes",
+           "lrsa_cache_append_quant", "lrsa_cache_read_quant", "lrsa_decode_attn_quant", "lrsa_decode_attn_quant_ws_bytes", "lrsa_cache_evict_quant",
            "lrsa_timing_enable", "lrsa_timing_count", "lrsa_timing_read")
 
 
@@ -36,6 +38,12 @@ class LrsaParams(ctypes.Structure):
         ("softmax_scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("impl", ctypes.c_int32),
         ("q_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3),
     ]
+
+
+class LrsaQuantCache(ctypes.Structure):
+    """Mirror of lrsa_quant_cache in include/lrsa.h."""
+    _fields_ = [("format", ctypes.c_int32), ("block", ctypes.c_int32), ("stride", ctypes.c_int64 * 3),
+                ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p)]
 
 
 class LrsaError(RuntimeError):
@@ -84,6 +92,19 @@ def lib() -> ctypes.CDLL:
         L.lrsa_attn_bwd_finish.argtypes = [vp, vp, vp, vp, vp, vp]
         L.lrsa_attn_fwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.lrsa_attn_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        f32 = ctypes.c_float
+        L.lrsa_decode_attn_acc_ws_bytes.restype = sz
+        L.lrsa_decode_attn_acc_ws_bytes.argtypes = [vp, i32]
+        L.lrsa_decode_attn_acc.argtypes = [vp, vp, vp, vp, i32, vp, vp, f32, vp, vp, vp, sz, vp]
+        L.lrsa_cache_evict_ws_bytes.restype = sz
+        L.lrsa_cache_evict_ws_bytes.argtypes = [vp, i32, i32]
+        L.lrsa_cache_evict.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.lrsa_cache_append_quant.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
+        L.lrsa_cache_read_quant.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp]
+        L.lrsa_decode_attn_quant_ws_bytes.restype = sz
+        L.lrsa_decode_attn_quant_ws_bytes.argtypes = [vp, i32, i32, ctypes.c_int]
+        L.lrsa_decode_attn_quant.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, f32, vp, vp, vp, sz, vp]
+        L.lrsa_cache_evict_quant.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -305,6 +326,195 @@ def lrsa_decode_attn_static(p: LrsaParams, q: torch.Tensor, Kc: torch.Tensor, Vc
     _check(lib().lrsa_decode_attn_static(ctypes.byref(p), _ptr(q), _ptr(Kc), _ptr(Vc), int(length), _ptr(O), _ptr(lse),
                                          _stream()))
     return O, lse
+
+
+# ---- accumulated weights, eviction, the cache in 8 bits
+def _here(device: torch.device) -> None:
+    """The library launches on the current device's current stream: tensors that live elsewhere are refused."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _call_ws(need: int, device, ws: Optional[torch.Tensor]) -> Tuple[Optional[torch.Tensor], int]:
+    if ws is None:
+        if need == 0:
+            return None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    elif ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on {device}")
+    return ws, ws.numel() * ws.element_size()
+
+
+def decode_attn_acc_ws_bytes(p: LrsaParams, length: int) -> int:
+    return int(lib().lrsa_decode_attn_acc_ws_bytes(ctypes.byref(p), int(length)))
+
+
+def lrsa_decode_attn_acc(p: LrsaParams, q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, length: int, acc_in: Optional[torch.Tensor],
+                         acc_out: torch.Tensor, decay: float = 1.0, O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None):
+    """lrsa_decode_attn that also writes acc_out = decay * acc_in + the weight that every cache row received, summed over the heads of
+    its group: acc [B, Hkv, cap] fp32, acc_in None for zeros, both may be the same tensor.  Returns (O, lse, acc_out)."""
+    dev, dt = q.device, _TORCH_DTYPE.get(p.dtype)
+    _here(dev)
+    if O is None:
+        O = torch.empty((p.batch, p.heads_q, p.head_dim), dtype=q.dtype, device=dev)
+    if lse is None:
+        lse = torch.empty((p.batch, p.heads_q), dtype=torch.float32, device=dev)
+    for name, t in (("q", q), ("O", O)):
+        _expect(name, t, (p.batch, p.heads_q, p.head_dim), None, dt, dev)
+    _expect("lse", lse, (p.batch, p.heads_q), None, torch.float32, dev)
+    _expect_kv(p, dev, Kc=Kc, Vc=Vc)
+    for name, t in (("acc_in", acc_in), ("acc_out", acc_out)):
+        _expect(name, t, (p.batch, p.heads_kv, p.seq), None, torch.float32, dev)
+    ws, nb = _call_ws(decode_attn_acc_ws_bytes(p, length), dev, ws)
+    _check(lib().lrsa_decode_attn_acc(ctypes.byref(p), _ptr(q), _ptr(Kc), _ptr(Vc), int(length), _ptr(acc_in), _ptr(acc_out), float(decay),
+                                      _ptr(O), _ptr(lse), _ptr(ws), nb, _stream()))
+    return O, lse, acc_out
+
+
+def cache_evict_ws_bytes(p: LrsaParams, length: int, budget: int) -> int:
+    """Workspace of lrsa_cache_evict, and of lrsa_cache_evict_quant with its max_len as the length."""
+    return int(lib().lrsa_cache_evict_ws_bytes(ctypes.byref(p), int(length), int(budget)))
+
+
+def _expect_lists(p: LrsaParams, dev, pos, acc, pos_o, acc_o) -> None:
+    for name, t, dt in (("pos", pos, torch.int32), ("acc", acc, torch.float32), ("pos_o", pos_o, torch.int32), ("acc_o", acc_o, torch.float32)):
+        _expect(name, t, (p.batch, p.heads_kv, p.seq), None, dt, dev)
+
+
+def lrsa_cache_evict(p: LrsaParams, Kc: torch.Tensor, Vc: torch.Tensor, pos: Optional[torch.Tensor], acc: torch.Tensor, length: int, budget: int,
+                     recent: int, Ko: torch.Tensor, Vo: torch.Tensor, pos_o: Optional[torch.Tensor], acc_o: torch.Tensor,
+                     ws: Optional[torch.Tensor] = None) -> int:
+    """The first p.sink rows, the last `recent` and those of the others with the largest acc, `budget` in all, go to the cache Ko, Vo
+    (with their positions and weights; weights behind them become zero).  Returns the new length."""
+    dev, new = Kc.device, ctypes.c_int32(0)
+    _here(dev)
+    _expect_kv(p, dev, Kc=Kc, Vc=Vc, Ko=Ko, Vo=Vo)
+    _expect_lists(p, dev, pos, acc, pos_o, acc_o)
+    ws, nb = _call_ws(cache_evict_ws_bytes(p, length, budget), dev, ws)
+    _check(lib().lrsa_cache_evict(ctypes.byref(p), _ptr(Kc), _ptr(Vc), _ptr(pos), _ptr(acc), int(length), int(budget), int(recent), _ptr(Ko),
+                                  _ptr(Vo), _ptr(pos_o), _ptr(acc_o), ctypes.byref(new), _ptr(ws), nb, _stream()))
+    return new.value
+
+
+_QUANT_FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+
+class QuantCache:
+    """The K and V of a cache in 8 bits: codes [B, Hkv, cap, d] (torch.int8 or torch.float8_e4m3fn, K and V by the same strides) and
+    fp32 scales [B, Hkv, ceil(cap / block)] of blocks of 16, 32, 64 or 128 rows.  Holds the tensors and the struct that the library reads."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: torch.Tensor, V_scale: torch.Tensor, block: int):
+        if K.dtype not in _QUANT_FORMATS:
+            raise ValueError(f"codes are torch.int8 or torch.float8_e4m3fn, not {K.dtype}")
+        if K.dim() != 4 or K.stride(3) != 1:
+            raise ValueError("codes are [B, Hkv, cap, d] with a channel stride of 1")
+        if block not in (16, 32, 64, 128):
+            raise ValueError(f"blocks of {block} rows are not built (16, 32, 64 and 128 are)")
+        B, Hkv, cap, _ = K.shape
+        _expect("V", V, K.shape, K.stride(), K.dtype, K.device)
+        for name, t in (("K_scale", K_scale), ("V_scale", V_scale)):
+            _expect(name, t, (B, Hkv, -(-cap // block)), None, torch.float32, K.device)
+        self.K, self.V, self.K_scale, self.V_scale, self.block = K, V, K_scale, V_scale, block
+        # the stride of an axis of length 1 is whatever torch made it: any multiple of 16 serves
+        st = [s if n > 1 else K.shape[3] for s, n in zip(K.stride()[:3], K.shape[:3])]
+        self.struct = LrsaQuantCache(_QUANT_FORMATS[K.dtype], block, (ctypes.c_int64 * 3)(*st), K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr())
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, B: int, Hkv: int, cap: int, d: int, dtype=torch.int8, block: int = 64, device="cuda") -> "QuantCache":
+        codes = [torch.zeros((B, Hkv, cap, d), dtype=torch.uint8, device=device).view(dtype) for _ in range(2)]
+        return cls(*codes, *(torch.ones((B, Hkv, -(-cap // block)), dtype=torch.float32, device=device) for _ in range(2)), block)
+
+
+def _expect_cache(p: LrsaParams, name: str, c: QuantCache, device) -> None:
+    """The tensors were checked when the cache was made; here that it is the one that the params describe."""
+    if tuple(c.K.shape) != (p.batch, p.heads_kv, p.seq, p.head_dim):
+        raise ValueError(f"{name}: codes {tuple(c.K.shape)}, the params describe {(p.batch, p.heads_kv, p.seq, p.head_dim)}")
+    if c.K.device != device:
+        raise ValueError(f"{name}: on {c.K.device}, expected {device}")
+
+
+def _expect_new_rows(p: LrsaParams, device, rows: int, **tensors) -> None:
+    for name, t in tensors.items():
+        _expect(name, t, (p.batch, p.heads_kv, rows, p.head_dim), (*p.kv_stride, 1), _TORCH_DTYPE.get(p.dtype), device)
+
+
+def lrsa_cache_append_quant(p: LrsaParams, cache: QuantCache, K: torch.Tensor, V: torch.Tensor, lens: torch.Tensor,
+                            counts: Optional[torch.Tensor] = None) -> None:
+    """Rows lens[b] .. of the cache become the first counts[b] (None: all) rows of K and V [B, Hkv, tokens, d], strides as p.kv_stride says;
+    lens, counts: [B] int32 on the device, not changed."""
+    dev = K.device
+    _here(dev)
+    _expect_cache(p, "cache", cache, dev)
+    tokens = K.shape[2]
+    _expect_new_rows(p, dev, tokens, K=K, V=V)
+    for name, t in (("lens", lens), ("counts", counts)):
+        _expect(name, t, (p.batch,), None, torch.int32, dev)
+    _check(lib().lrsa_cache_append_quant(ctypes.byref(p), cache.ref, _ptr(K), _ptr(V), tokens, _ptr(lens), _ptr(counts), _stream()))
+
+
+def lrsa_cache_read_quant(p: LrsaParams, cache: QuantCache, lens: torch.Tensor, rows: int, first: Optional[torch.Tensor] = None,
+                          K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
+    """Rows first[b] (None: 0) .. + rows of every sequence as values [B, Hkv, rows, d], zero at and behind lens[b]; returns (K, V), by
+    default of the strides that p.kv_stride gives."""
+    dev, dt = cache.K.device, _TORCH_DTYPE.get(p.dtype)
+    _here(dev)
+    _expect_cache(p, "cache", cache, dev)
+    rows = int(rows)
+    K, V = (torch.empty_strided((p.batch, p.heads_kv, rows, p.head_dim), (*p.kv_stride, 1), dtype=dt, device=dev) if t is None else t for t in (K, V))
+    _expect_new_rows(p, dev, rows, K=K, V=V)
+    for name, t in (("lens", lens), ("first", first)):
+        _expect(name, t, (p.batch,), None, torch.int32, dev)
+    _check(lib().lrsa_cache_read_quant(ctypes.byref(p), cache.ref, _ptr(lens), rows, _ptr(first), _ptr(K), _ptr(V), _stream()))
+    return K, V
+
+
+def decode_attn_quant_ws_bytes(p: LrsaParams, tokens: int, max_len: int, with_acc: bool) -> int:
+    return int(lib().lrsa_decode_attn_quant_ws_bytes(ctypes.byref(p), int(tokens), int(max_len), 1 if with_acc else 0))
+
+
+def lrsa_decode_attn_quant(p: LrsaParams, q: torch.Tensor, cache: QuantCache, lens: torch.Tensor, max_len: int, acc_in: Optional[torch.Tensor] = None,
+                           acc_out: Optional[torch.Tensor] = None, decay: float = 1.0, O: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Attention of the last tokens of every sequence over the cache: q, O [B, Hq, tokens, d] (or [B, Hq, d]: one token), lens [B] int32 on
+    the device, none above max_len; token t sees the rows below lens[b] - tokens + 1 + t.  With acc_out, the rows' weights are added up
+    as in lrsa_decode_attn_acc.  Returns (O, lse [B, Hq, tokens] fp32)."""
+    dev, dt = q.device, _TORCH_DTYPE.get(p.dtype)
+    _here(dev)
+    _expect_cache(p, "cache", cache, dev)
+    tokens = q.shape[2] if q.dim() == 4 else 1
+    shape = (p.batch, p.heads_q, tokens, p.head_dim) if q.dim() == 4 else (p.batch, p.heads_q, p.head_dim)
+    if O is None:
+        O = torch.empty(shape, dtype=q.dtype, device=dev)
+    if lse is None:
+        lse = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
+    for name, t in (("q", q), ("O", O)):
+        _expect(name, t, shape, None, dt, dev)
+    _expect("lse", lse, shape[:-1], None, torch.float32, dev)
+    _expect("lens", lens, (p.batch,), None, torch.int32, dev)
+    for name, t in (("acc_in", acc_in), ("acc_out", acc_out)):
+        _expect(name, t, (p.batch, p.heads_kv, p.seq), None, torch.float32, dev)
+    ws, nb = _call_ws(decode_attn_quant_ws_bytes(p, tokens, max_len, acc_out is not None), dev, ws)
+    _check(lib().lrsa_decode_attn_quant(ctypes.byref(p), cache.ref, _ptr(q), tokens, _ptr(lens), int(max_len), _ptr(acc_in), _ptr(acc_out),
+                                        float(decay), _ptr(O), _ptr(lse), _ptr(ws), nb, _stream()))
+    return O, lse
+
+
+def lrsa_cache_evict_quant(p: LrsaParams, cache: QuantCache, pos: Optional[torch.Tensor], acc: torch.Tensor, lens: torch.Tensor, max_len: int,
+                           budget: int, recent: int, out: QuantCache, pos_o: Optional[torch.Tensor], acc_o: torch.Tensor, lens_o: torch.Tensor,
+                           ws: Optional[torch.Tensor] = None) -> None:
+    """lrsa_cache_evict from one cache in 8 bits to another of the same format and block; lens -> lens_o, [B] int32 on the device."""
+    dev = acc.device
+    _here(dev)
+    _expect_cache(p, "cache", cache, dev)
+    _expect_cache(p, "out", out, dev)
+    _expect_lists(p, dev, pos, acc, pos_o, acc_o)
+    for name, t in (("lens", lens), ("lens_o", lens_o)):
+        _expect(name, t, (p.batch,), None, torch.int32, dev)
+    ws, nb = _call_ws(cache_evict_ws_bytes(p, max_len, budget), dev, ws)
+    _check(lib().lrsa_cache_evict_quant(ctypes.byref(p), cache.ref, _ptr(pos), _ptr(acc), _ptr(lens), int(max_len), int(budget), int(recent),
+                                        out.ref, _ptr(pos_o), _ptr(acc_o), _ptr(lens_o), _ptr(ws), nb, _stream()))
 
 
 def lrsa_attn_fwd(p: LrsaParams, Q, K, V, idx, O: Optional[torch.Tensor] = None,

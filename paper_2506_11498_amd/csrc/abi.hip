@@ -2,6 +2,7 @@
 // and dispatch to the kernel launchers.  Declarations and contracts are in include/lrsa.h.
 #include "../../include/lrsa.h"
 #include "common.h"
+#include "quant_block.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -460,6 +461,179 @@ int lrsa_attn_bwd_finish(const lrsa_params* p, const float* dK_acc, const float*
     if (!fill_supported(p, D)) return fail(LRSA_ERR_UNSUPPORTED, "lrsa_attn_bwd_finish is built for bf16 with head_dim 128");
     if (!dK_acc || !dV_acc || !dK || !dV) return fail(LRSA_ERR_INVALID_ARG, "lrsa_attn_bwd_finish: pointers must not be NULL");
     return hip_result(lrsa::launch_bwd_acc_finish(D, dK_acc, dV_acc, dK, dV, (hipStream_t)stream), "lrsa_attn_bwd_finish");
+}
+
+}  // extern "C"
+
+// ---- accumulated weights, eviction, the cache in 8 bits
+namespace {
+
+int check_ws_bytes(const char* who, size_t need, const void* ws, size_t ws_bytes) {
+    if (need == 0) return LRSA_OK;
+    if (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % 256 != 0)
+        return fail(LRSA_ERR_INVALID_ARG, "%s: a 256-byte aligned workspace of %zu bytes is needed", who, need);
+    return LRSA_OK;
+}
+
+int check_acc(const char* who, const float* acc_in, const float* acc_out, float decay) {
+    if (acc_in && !acc_out) return fail(LRSA_ERR_INVALID_ARG, "%s: acc_in without acc_out", who);
+    if (!std::isfinite(decay)) return fail(LRSA_ERR_INVALID_ARG, "%s: decay is not finite", who);
+    return LRSA_OK;
+}
+
+int make_quant(const char* who, const lrsa::Dims& D, const lrsa_quant_cache* c, lrsa::QuantDims* Q) {
+    if (!c) return fail(LRSA_ERR_INVALID_ARG, "%s: the cache is NULL", who);
+    if (c->format != LRSA_QUANT_INT8 && c->format != LRSA_QUANT_E4M3) return fail(LRSA_ERR_UNSUPPORTED, "%s: format %d is not built", who, c->format);
+    if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128)
+        return fail(LRSA_ERR_UNSUPPORTED, "%s: blocks of %d rows are not built (16, 32, 64 and 128 are)", who, c->block);
+    if (!c->K || !c->V || !c->K_scale || !c->V_scale) return fail(LRSA_ERR_INVALID_ARG, "%s: the cache's pointers must not be NULL", who);
+    if (misaligned16(c->K) || misaligned16(c->V)) return fail(LRSA_ERR_INVALID_ARG, "%s: codes must be 16-byte aligned", who);
+    if (reinterpret_cast<uintptr_t>(c->K_scale) % 4 || reinterpret_cast<uintptr_t>(c->V_scale) % 4)
+        return fail(LRSA_ERR_INVALID_ARG, "%s: scales must be 4-byte aligned", who);
+    if (c->stride[2] < D.d) return fail(LRSA_ERR_INVALID_ARG, "%s: row stride %lld < head_dim", who, (long long)c->stride[2]);
+    for (int i = 0; i < 3; ++i)
+        if (c->stride[i] < 0 || c->stride[i] % 16 != 0)
+            return fail(LRSA_ERR_INVALID_ARG, "%s: stride %lld of the codes is negative or no multiple of 16", who, (long long)c->stride[i]);
+    Q->fmt = c->format == LRSA_QUANT_INT8 ? lrsa::QUANT_INT8 : lrsa::QUANT_E4M3;
+    Q->block = c->block;
+    Q->log_block = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
+    Q->nb = (int)(((int64_t)D.n + c->block - 1) / c->block);
+    for (int i = 0; i < 3; ++i) Q->st[i] = c->stride[i];
+    Q->K = (uint8_t*)c->K; Q->V = (uint8_t*)c->V;
+    Q->Ks = c->K_scale; Q->Vs = c->V_scale;
+    return LRSA_OK;
+}
+
+int check_evict(const char* who, const lrsa::Dims& D, int32_t len, int32_t budget, int32_t recent) {
+    if (len < 0 || len > D.n) return fail(LRSA_ERR_INVALID_ARG, "%s: length %d outside [0, cap=%d]", who, len, D.n);
+    if (recent < 0 || budget < 1 || budget > D.n || (int64_t)D.S + recent > budget)
+        return fail(LRSA_ERR_INVALID_ARG, "%s: budget %d must be in [1, cap=%d] and hold sink %d and recent %d", who, budget, D.n, D.S, recent);
+    if (!lrsa::cache_evict_grid_fits(D, budget)) return fail(LRSA_ERR_UNSUPPORTED, "%s: budget %d is beyond the launch grid limits", who, budget);
+    return LRSA_OK;
+}
+int check_evict_lists(const char* who, const int32_t* pos, const float* acc, const int32_t* pos_o, const float* acc_o) {
+    if (!acc || !acc_o) return fail(LRSA_ERR_INVALID_ARG, "%s: acc and acc_o must not be NULL", who);
+    if (!pos != !pos_o) return fail(LRSA_ERR_INVALID_ARG, "%s: pos and pos_o go together", who);
+    if (acc == acc_o || (pos && pos == pos_o)) return fail(LRSA_ERR_INVALID_ARG, "%s: the new lists must not be the old ones", who);
+    return LRSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lrsa_decode_attn_acc_ws_bytes(const lrsa_params* p, int32_t len) {
+    lrsa::Dims D;
+    return make_dims(p, &D) == LRSA_OK && len >= 1 && len <= D.n ? lrsa::decode_acc_ws_bytes(D, len) : 0;
+}
+
+int lrsa_decode_attn_acc(const lrsa_params* p, const void* q, const void* Kc, const void* Vc, int32_t len, const float* acc_in, float* acc_out,
+                         float decay, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    static const char* who = "lrsa_decode_attn_acc";
+    lrsa::Dims D;
+    int rc = make_dims(p, &D);
+    if (rc != LRSA_OK) return rc;
+    if (len < 1 || len > D.n) return fail(LRSA_ERR_INVALID_ARG, "%s: len %d outside [1, cap=%d]", who, len, D.n);
+    if (!q || !Kc || !Vc || !O || !acc_out) return fail(LRSA_ERR_INVALID_ARG, "%s: q, Kc, Vc, O and acc_out must not be NULL", who);
+    if (misaligned16(q) || misaligned16(Kc) || misaligned16(Vc)) return fail(LRSA_ERR_INVALID_ARG, "%s: q, Kc and Vc must be 16-byte aligned", who);
+    if ((rc = check_acc(who, acc_in, acc_out, decay)) != LRSA_OK) return rc;
+    if (!lrsa::decode_acc_grid_fits(D, len)) return fail(LRSA_ERR_UNSUPPORTED, "%s: batch * heads or len beyond the launch grid limits", who);
+    if ((rc = check_ws_bytes(who, lrsa::decode_acc_ws_bytes(D, len), ws, ws_bytes)) != LRSA_OK) return rc;
+    return hip_result(lrsa::launch_decode_attn_acc(D, q, Kc, Vc, len, O, lse, acc_in, acc_out, decay, ws, (hipStream_t)stream), who);
+}
+
+size_t lrsa_cache_evict_ws_bytes(const lrsa_params* p, int32_t len, int32_t budget) {
+    lrsa::Dims D;
+    return make_dims(p, &D) == LRSA_OK && check_evict("lrsa_cache_evict_ws_bytes", D, len, budget, 0) == LRSA_OK ? lrsa::cache_evict_ws_bytes(D, budget) : 0;
+}
+
+int lrsa_cache_evict(const lrsa_params* p, const void* Kc, const void* Vc, const int32_t* pos, const float* acc, int32_t len, int32_t budget,
+                     int32_t recent, void* Ko, void* Vo, int32_t* pos_o, float* acc_o, int32_t* len_out, void* ws, size_t ws_bytes, void* stream) {
+    static const char* who = "lrsa_cache_evict";
+    lrsa::Dims D;
+    int rc = make_dims(p, &D);
+    if (rc != LRSA_OK) return rc;
+    if (!len_out) return fail(LRSA_ERR_INVALID_ARG, "%s: len_out must not be NULL", who);
+    if ((rc = check_evict(who, D, len, budget, recent)) != LRSA_OK) return rc;
+    if (!Kc || !Vc || !Ko || !Vo) return fail(LRSA_ERR_INVALID_ARG, "%s: Kc, Vc, Ko and Vo must not be NULL", who);
+    if (misaligned16(Kc) || misaligned16(Vc) || misaligned16(Ko) || misaligned16(Vo))
+        return fail(LRSA_ERR_INVALID_ARG, "%s: Kc, Vc, Ko and Vo must be 16-byte aligned", who);
+    if (Ko == Kc || Vo == Vc || Ko == Vc || Vo == Kc || Ko == Vo) return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must not be the old one", who);
+    if ((rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
+    if ((rc = check_ws_bytes(who, lrsa::cache_evict_ws_bytes(D, budget), ws, ws_bytes)) != LRSA_OK) return rc;
+    rc = hip_result(lrsa::launch_cache_evict(D, Kc, Vc, pos, acc, len, budget, recent, Ko, Vo, pos_o, acc_o, ws, (hipStream_t)stream), who);
+    if (rc == LRSA_OK) *len_out = len < budget ? len : budget;
+    return rc;
+}
+
+int lrsa_cache_append_quant(const lrsa_params* p, const lrsa_quant_cache* c, const void* K, const void* V, int32_t tokens, const int32_t* lens,
+                            const int32_t* counts, void* stream) {
+    static const char* who = "lrsa_cache_append_quant";
+    lrsa::Dims D;
+    lrsa::QuantDims Q;
+    int rc = make_dims(p, &D);
+    if (rc != LRSA_OK || (rc = make_quant(who, D, c, &Q)) != LRSA_OK) return rc;
+    if (tokens < 1) return fail(LRSA_ERR_INVALID_ARG, "%s: tokens must be >= 1", who);
+    if (!K || !V || !lens) return fail(LRSA_ERR_INVALID_ARG, "%s: K, V and lens must not be NULL", who);
+    if (misaligned16(K) || misaligned16(V)) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
+    if (!lrsa::grid_fits(Q.nb, 256)) return fail(LRSA_ERR_UNSUPPORTED, "%s: cap %d is beyond the launch grid limits", who, D.n);
+    return hip_result(lrsa::launch_append_quant(D, Q, K, V, tokens, lens, counts, (hipStream_t)stream), who);
+}
+
+int lrsa_cache_read_quant(const lrsa_params* p, const lrsa_quant_cache* c, const int32_t* lens, int32_t rows, const int32_t* first, void* K, void* V,
+                          void* stream) {
+    static const char* who = "lrsa_cache_read_quant";
+    lrsa::Dims D;
+    lrsa::QuantDims Q;
+    int rc = make_dims(p, &D);
+    if (rc != LRSA_OK || (rc = make_quant(who, D, c, &Q)) != LRSA_OK) return rc;
+    if (rows < 1) return fail(LRSA_ERR_INVALID_ARG, "%s: rows must be >= 1", who);
+    if (!K || !V || !lens) return fail(LRSA_ERR_INVALID_ARG, "%s: K, V and lens must not be NULL", who);
+    if (misaligned16(K) || misaligned16(V)) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
+    if (!lrsa::read_quant_grid_fits(D, rows)) return fail(LRSA_ERR_UNSUPPORTED, "%s: rows %d are beyond the launch grid limits", who, rows);
+    return hip_result(lrsa::launch_read_quant(D, Q, lens, rows, first, K, V, (hipStream_t)stream), who);
+}
+
+size_t lrsa_decode_attn_quant_ws_bytes(const lrsa_params* p, int32_t tokens, int32_t max_len, int with_acc) {
+    lrsa::Dims D;
+    if (make_dims(p, &D) != LRSA_OK || tokens < 1 || tokens > 16 || max_len < 1 || max_len > D.n) return 0;
+    return lrsa::decode_quant_ws_bytes(D, tokens, max_len, with_acc != 0);
+}
+
+int lrsa_decode_attn_quant(const lrsa_params* p, const lrsa_quant_cache* c, const void* q, int32_t tokens, const int32_t* lens, int32_t max_len,
+                           const float* acc_in, float* acc_out, float decay, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    static const char* who = "lrsa_decode_attn_quant";
+    lrsa::Dims D;
+    lrsa::QuantDims Q;
+    int rc = make_dims(p, &D);
+    if (rc != LRSA_OK || (rc = make_quant(who, D, c, &Q)) != LRSA_OK) return rc;
+    if (tokens < 1 || tokens > 16) return fail(LRSA_ERR_INVALID_ARG, "%s: tokens %d outside [1, 16]", who, tokens);
+    if (max_len < 1 || max_len > D.n) return fail(LRSA_ERR_INVALID_ARG, "%s: max_len %d outside [1, cap=%d]", who, max_len, D.n);
+    if (!q || !lens || !O) return fail(LRSA_ERR_INVALID_ARG, "%s: q, lens and O must not be NULL", who);
+    if (misaligned16(q)) return fail(LRSA_ERR_INVALID_ARG, "%s: q must be 16-byte aligned", who);
+    if ((rc = check_acc(who, acc_in, acc_out, decay)) != LRSA_OK) return rc;
+    if (!lrsa::decode_quant_grid_fits(D, tokens, max_len))
+        return fail(LRSA_ERR_UNSUPPORTED, "%s: batch * heads * tokens or max_len beyond the launch grid limits", who);
+    if ((rc = check_ws_bytes(who, lrsa::decode_quant_ws_bytes(D, tokens, max_len, acc_out != nullptr), ws, ws_bytes)) != LRSA_OK) return rc;
+    return hip_result(lrsa::launch_decode_quant(D, Q, q, tokens, lens, max_len, O, lse, acc_in, acc_out, decay, ws, (hipStream_t)stream), who);
+}
+
+int lrsa_cache_evict_quant(const lrsa_params* p, const lrsa_quant_cache* c, const int32_t* pos, const float* acc, const int32_t* lens, int32_t max_len,
+                           int32_t budget, int32_t recent, const lrsa_quant_cache* o, int32_t* pos_o, float* acc_o, int32_t* lens_o, void* ws,
+                           size_t ws_bytes, void* stream) {
+    static const char* who = "lrsa_cache_evict_quant";
+    lrsa::Dims D;
+    lrsa::QuantDims Q, N;
+    int rc = make_dims(p, &D);
+    if (rc != LRSA_OK || (rc = make_quant(who, D, c, &Q)) != LRSA_OK || (rc = make_quant(who, D, o, &N)) != LRSA_OK) return rc;
+    if (Q.fmt != N.fmt || Q.block != N.block) return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must have the format and block of the old one", who);
+    if ((rc = check_evict(who, D, max_len, budget, recent)) != LRSA_OK) return rc;
+    if (Q.K == N.K || Q.V == N.V || Q.K == N.V || Q.V == N.K || N.K == N.V || Q.Ks == N.Ks || Q.Vs == N.Vs || Q.Ks == N.Vs || Q.Vs == N.Ks || N.Ks == N.Vs)
+        return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must not be the old one", who);
+    if (!lens || !lens_o || lens == lens_o) return fail(LRSA_ERR_INVALID_ARG, "%s: lens and lens_o must be two arrays", who);
+    if ((rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
+    if ((rc = check_ws_bytes(who, lrsa::cache_evict_ws_bytes(D, budget), ws, ws_bytes)) != LRSA_OK) return rc;
+    return hip_result(lrsa::launch_cache_evict_quant(D, Q, N, lens, max_len, budget, recent, pos, acc, pos_o, acc_o, lens_o, ws, (hipStream_t)stream), who);
 }
 
 }  // extern "C"

@@ -67,6 +67,28 @@ constexpr size_t DECODE_STATIC_SCRATCH_BYTES = size_t(4) << 20;
 size_t decode_static_need(const Dims&, int len);
 hipError_t launch_decode_attn_static(const Dims&, const void* q, const void* Kc, const void* Vc, int len, void* O,
                                      float* lse, hipStream_t st);
+// the same attention with the rows' weights added to acc (lrsa_decode_attn_acc)
+size_t decode_acc_ws_bytes(const Dims&, int len);
+bool decode_acc_grid_fits(const Dims&, int len);
+hipError_t launch_decode_attn_acc(const Dims&, const void* q, const void* Kc, const void* Vc, int len, void* O, float* lse, const float* acc_in,
+                                  float* acc_out, float decay, void* ws, hipStream_t st);
+// eviction by accumulated weight
+size_t cache_evict_ws_bytes(const Dims&, int budget);
+bool cache_evict_grid_fits(const Dims&, int budget);
+hipError_t launch_cache_evict(const Dims&, const void* K, const void* V, const int32_t* pos, const float* acc, int len, int budget, int recent,
+                              void* Ko, void* Vo, int32_t* pos_o, float* acc_o, void* ws, hipStream_t st);
+// the cache in 8 bits
+struct QuantDims;
+hipError_t launch_append_quant(const Dims&, const QuantDims&, const void* K, const void* V, int tokens, const int32_t* lens, const int32_t* counts,
+                               hipStream_t st);
+bool read_quant_grid_fits(const Dims&, int rows);
+hipError_t launch_read_quant(const Dims&, const QuantDims&, const int32_t* lens, int rows, const int32_t* first, void* K, void* V, hipStream_t st);
+size_t decode_quant_ws_bytes(const Dims&, int tokens, int max_len, bool acc);
+bool decode_quant_grid_fits(const Dims&, int tokens, int max_len);
+hipError_t launch_decode_quant(const Dims&, const QuantDims&, const void* q, int tokens, const int32_t* lens, int max_len, void* O, float* lse,
+                               const float* acc_in, float* acc_out, float decay, void* ws, hipStream_t st);
+hipError_t launch_cache_evict_quant(const Dims&, const QuantDims& from, const QuantDims& to, const int32_t* lens, int max_len, int budget, int recent,
+                                    const int32_t* pos, const float* acc, int32_t* pos_o, float* acc_o, int32_t* lens_o, void* ws, hipStream_t st);
 hipError_t launch_score_select(const Dims&, const void* K, const void* V, float* score, int32_t* idx, void* ws, hipStream_t st);
 
 size_t attn_fwd_generic_ws_bytes(const Dims&);

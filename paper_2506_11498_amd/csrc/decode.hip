@@ -14,7 +14,10 @@
 //                   slice of the cache rows, bf16, on the matrix cores: fp32 online softmax, partial (max, sum,
 //                   output) per slice;
 // k_decode_attn     the same for fp32 data, in the vector pipe;
-// k_decode_combine  merges the slices.
+// k_decode_combine  merges the slices;
+// k_decode_combine_acc  the same, and adds the weights that the cache rows received to their accumulated weights
+//                   (lrsa_decode_attn_acc), from the logits that the kernels above then leave in the workspace.
+#include "decode_merge.h"
 #include "mfma_tiles.h"
 #include "score_block.h"
 #include "select_block.h"
@@ -23,10 +26,7 @@
 
 namespace lrsa {
 
-constexpr int DEC_THREADS = 256;
-constexpr int DEC_WAVES = DEC_THREADS / 64;
 constexpr int DEC_GMAX = 8;            // query heads of a group handled per pass
-constexpr int DEC_MAX_SPLITS = 256;
 constexpr int DEC_U = 4;               // rows per lane group and step
 constexpr int DEC_TILE = 32;           // rows per wave and step of k_decode_mfma
 
@@ -45,11 +45,14 @@ static size_t part_bytes(const Dims& D, int splits) { return size_t(D.B) * D.Hq 
 // A call that the scratch of lrsa_decode_attn_static held with decode_static_splits still fits: beyond it the slices stay at that
 // number, in both calls, so that they give the same bits (more of them are no gain there: bf16, 512 units of 16 heads, 8K rows
 // 356 us, 378 with four slices; 2K rows 124 and 114 us).
-static int decode_splits(const Dims& D, int len) {
+static int decode_fine_splits(const Dims& D, int len) {
     const int units = D.B * D.Hkv, most = (len + 127) / 128;
     int s = units <= 128 ? 512 / units : 2048 / units;
     s = s < most ? s : most;
-    s = s < 1 ? 1 : s > DEC_MAX_SPLITS ? DEC_MAX_SPLITS : s;
+    return s < 1 ? 1 : s > DEC_MAX_SPLITS ? DEC_MAX_SPLITS : s;
+}
+static int decode_splits(const Dims& D, int len) {
+    const int units = D.B * D.Hkv, s = decode_fine_splits(D, len);
     const int base = decode_static_splits(D, len);
     if (D.dtype == 0 && D.G > 2 && units > (D.G == 3 ? 128 : 84)) return base;
     return s > base && part_bytes(D, s) > DECODE_STATIC_SCRATCH_BYTES ? base : s;
@@ -313,15 +316,6 @@ hipError_t launch_cache_compress_ws(const Dims& D, void* Kc, void* Vc, int32_t* 
 }
 
 // ------------------------------------------------------------------------------------ single-query attention
-// (m, l, o) of two disjoint key sets -> of their union
-__device__ __forceinline__ void merge_state(float& m, float& l, float m2, float l2, float& a, float& b2) {
-    const float mn = fmaxf(m, m2);
-    a = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
-    b2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - mn);
-    l = l * a + l2 * b2;
-    m = mn;
-}
-
 // bf16.  One workgroup: the heads of one KV group (16 at a time) x rows [split * per, ...) of the cache; its waves take tiles
 // of 32 rows in turn.  Nothing is staged in LDS.  Lane l, c = l % 16, q4 = l / 16, v_mfma_f32_16x16x32_bf16:
 //   S = K Q^T   row m of block kb is tile row 8*(m/4) + 4*kb + m%4, column c a head: the lane then holds the logits of tile
@@ -354,8 +348,9 @@ template <int DH> struct DecState {
     float m, l;          // of head c; l over the lane's own rows
     f32x4 o[DH / 16];
 };
-template <int DH>
-__device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t, const bf16x8 (&qf)[DH / 32], int r, int r1, float c2) {
+// LOGITS: `logits` is where the lane's 8 logits of the tile go, or NULL
+template <int DH, bool LOGITS>
+__device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t, const bf16x8 (&qf)[DH / 32], int r, int r1, float c2, float* logits) {
     f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
     for (int kk = 0; kk < DH / 32; ++kk)
@@ -366,6 +361,12 @@ __device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t,
     for (int j = 0; j < 8; ++j) {
         p[j] = r + j < r1 ? s[j >> 2][j & 3] * c2 : -INFINITY;
         mx = fmaxf(mx, p[j]);
+    }
+    if constexpr (LOGITS) {
+        if (logits) {      // before the factor c2: the arithmetic on p stays as it is without the stores
+            reinterpret_cast<f32x4*>(logits)[0] = s[0];
+            reinterpret_cast<f32x4*>(logits)[1] = s[1];
+        }
     }
     lanes_u32x2 x = pair32(__float_as_uint(mx));
     mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
@@ -406,10 +407,10 @@ __device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t,
     }
 }
 
-template <int DH>
+template <int DH, bool LOGITS>
 __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf16_t* __restrict__ q, const bf16_t* __restrict__ Kc,
                                                                 const bf16_t* __restrict__ Vc, int len, int per, int splits,
-                                                                float* __restrict__ part) {
+                                                                float* __restrict__ part, float* __restrict__ logits, int64_t lstride) {
     constexpr int CPL = DH / 16, LROW = DH + 4;              // channels per lane; the padding spreads the heads over the banks
     __shared__ __attribute__((aligned(16))) float sO[DEC_WAVES][16][LROW];
     __shared__ float sM[DEC_WAVES][16], sL[DEC_WAVES][16];
@@ -435,15 +436,21 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
         // the next tile's loads are in flight while a tile is used
         constexpr int STEP = DEC_WAVES * DEC_TILE;
         int r = r0 + wave * DEC_TILE;
+        // tiles begin at multiples of 32 rows, and so does the end of the rows that lstride has room for
+        float* lrow = nullptr;
+        if constexpr (LOGITS) {
+            if (c < gn) lrow = logits + (int64_t(b) * D.Hq + h * D.G + g0 + c) * lstride + vr;
+        }
+        auto at = [&](int row) { return LOGITS && lrow ? lrow + row : nullptr; };
         if (r < r1) {
             DecTile<DH> A, B;
             load_tile<DH>(A, Kl, Vl, D.ks[2], r + kr, r + vr, r1 - 1);
             for (;;) {
                 if (r + STEP < r1) load_tile<DH>(B, Kl, Vl, D.ks[2], r + STEP + kr, r + STEP + vr, r1 - 1);
-                use_tile<DH>(st, A, qf, r + vr, r1, c2);
+                use_tile<DH, LOGITS>(st, A, qf, r + vr, r1, c2, at(r));
                 if ((r += STEP) >= r1) break;
                 if (r + STEP < r1) load_tile<DH>(A, Kl, Vl, D.ks[2], r + STEP + kr, r + STEP + vr, r1 - 1);
-                use_tile<DH>(st, B, qf, r + vr, r1, c2);
+                use_tile<DH, LOGITS>(st, B, qf, r + vr, r1, c2, at(r));
                 if ((r += STEP) >= r1) break;
             }
         }
@@ -479,10 +486,10 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
 
 // fp32.  One workgroup: the G heads of one KV group (DEC_GMAX at a time) x rows [r0, r1) of the cache.  A row is
 // spread over lpr = 16-byte pieces; a wave reads 64 / lpr rows per step; logits are kept in log2 units.
-template <typename T>
+template <typename T, bool LOGITS>
 __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __restrict__ q, const T* __restrict__ Kc,
                                                              const T* __restrict__ Vc, int len, int splits,
-                                                             float* __restrict__ part) {
+                                                             float* __restrict__ part, float* __restrict__ logits, int64_t lstride) {
     constexpr int VEC = Elem<T>::VEC;
     const int lpr = D.d / VEC, rpw = 64 / lpr;
     const int split = blockIdx.x, bh = blockIdx.y, b = bh / D.Hkv, h = bh % D.Hkv;
@@ -530,6 +537,14 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __
                 for (int off = lpr >> 1; off > 0; off >>= 1)
 #pragma unroll
                     for (int u = 0; u < DEC_U; ++u) sc[u] += __shfl_xor(sc[u], off, 64);
+                if constexpr (LOGITS) {
+                    if (sub == 0) {      // before the factor c2: the arithmetic below stays as it is without the stores
+                        float* dst = logits + (int64_t(b) * D.Hq + h * D.G + g0 + g) * lstride + rb;
+#pragma unroll
+                        for (int u = 0; u < DEC_U; ++u)
+                            if (rb + u * step < r1) dst[u * step] = sc[u];
+                    }
+                }
 #pragma unroll
                 for (int u = 0; u < DEC_U; ++u) {
                     sc[u] = rb + u * step < r1 ? sc[u] * c2 : -INFINITY;
@@ -584,63 +599,29 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __
     }
 }
 
-// One (batch, query head) per workgroup: the weights of all slices first (two loads per lane and 64 slices), then the
-// records are summed by all lanes, two channels each, COMB_U loads in flight; fixed order.
-constexpr int COMB_U = 4;
+// One (batch, query head) per workgroup.
 template <typename T>
 __global__ __launch_bounds__(DEC_THREADS) void k_decode_combine(Dims D, const float* __restrict__ part, int splits,
                                                                 T* __restrict__ O, float* __restrict__ lse) {
-    __shared__ float sW[DEC_MAX_SPLITS];
-    __shared__ float2 sO[DEC_THREADS];
+    __shared__ CombineLds sh;
     const int64_t bhq = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, rec = D.d + 2;
-    const float* src = part + bhq * splits * rec;
-    float m[DEC_MAX_SPLITS / 64], l[DEC_MAX_SPLITS / 64], M = -INFINITY, L = 0.0f;
-#pragma unroll
-    for (int i = 0; i < DEC_MAX_SPLITS / 64; ++i) {
-        const int s = lane + 64 * i;
-        m[i] = -INFINITY; l[i] = 0.0f;
-        if (s < splits) {
-            const float2 ml = *reinterpret_cast<const float2*>(src + int64_t(s) * rec);
-            m[i] = ml.x; l[i] = ml.y;
-        }
-        M = fmaxf(M, m[i]);
+    combine_row<T>(part + bhq * splits * (D.d + 2), D.d, splits, O + bhq * D.d, lse ? lse + bhq : nullptr, sh);
+}
+
+// The first B * Hq workgroups as above, the others: ACC_ROWS cache rows of a unit each.  One launch, because the two need
+// the same records and do not wait for each other.
+template <typename T>
+__global__ __launch_bounds__(DEC_THREADS) void k_decode_combine_acc(Dims D, const float* __restrict__ part, int splits, T* __restrict__ O,
+                                                                    float* __restrict__ lse, AccArgs A, int len, int chunks) {
+    __shared__ union { CombineLds c; float lse[ACC_COLS]; } sh;
+    const int rec = D.d + 2, rows = D.B * D.Hq;
+    if (int(blockIdx.x) < rows) {
+        const int64_t bhq = blockIdx.x;
+        combine_row<T>(part + bhq * splits * rec, D.d, splits, O + bhq * D.d, lse ? lse + bhq : nullptr, sh.c);
+        return;
     }
-    M = wave_max(M);
-#pragma unroll
-    for (int i = 0; i < DEC_MAX_SPLITS / 64; ++i) {
-        const float w = m[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[i] - M);
-        L = __builtin_fmaf(l[i], w, L);
-        if (tid < 64) sW[lane + 64 * i] = w;
-    }
-    L = wave_sum(L);
-    __syncthreads();
-    const int pairs = D.d / 2, ways = DEC_THREADS / pairs, ch = tid % pairs, way = tid / pairs;
-    float2 o = {0.0f, 0.0f};
-    for (int s0 = way; s0 < splits; s0 += COMB_U * ways) {
-        float2 v[COMB_U];
-        float w[COMB_U];
-#pragma unroll
-        for (int u = 0; u < COMB_U; ++u) {
-            const int s = s0 + u * ways, sc = min(s, splits - 1);
-            w[u] = s < splits ? sW[sc] : 0.0f;
-            v[u] = *reinterpret_cast<const float2*>(src + int64_t(sc) * rec + 2 + 2 * ch);
-        }
-#pragma unroll
-        for (int u = 0; u < COMB_U; ++u) {
-            o.x = __builtin_fmaf(w[u], v[u].x, o.x);
-            o.y = __builtin_fmaf(w[u], v[u].y, o.y);
-        }
-    }
-    sO[tid] = o;
-    __syncthreads();
-    if (tid < pairs) {
-        for (int w = 1; w < ways; ++w) { o.x += sO[w * pairs + tid].x; o.y += sO[w * pairs + tid].y; }
-        Elem<T>::put(O + bhq * D.d + 2 * ch, o.x / L);
-        Elem<T>::put(O + bhq * D.d + 2 * ch + 1, o.y / L);
-        if (lse && tid == 0)   // one rounding at the end: ln 2 as its fp32 value plus the rest
-            lse[bhq] = __builtin_fmaf(M, 0.69314718246459961f, __builtin_fmaf(M, -1.9046542e-9f, __builtin_log2f(L) * 0.6931471805599453f));
-    }
+    const int at = int(blockIdx.x) - rows, unit = at / chunks;
+    acc_rows(A, unit, part + int64_t(unit) * D.G * splits * rec, int64_t(splits) * rec, rec, splits, at % chunks * ACC_ROWS, len, sh.lse);
 }
 
 // ------------------------------------------------------------------------------------ no-allocation variant
@@ -690,25 +671,72 @@ hipError_t launch_decode_attn_static(const Dims& D, const void* q, const void* K
     return launch_decode_attn(D, q, Kc, Vc, len, O, lse, part, st);
 }
 
+// the slices' records, and with LOGITS the logits
+template <bool LOGITS>
+static void decode_slices(const Dims& D, const void* q, const void* Kc, const void* Vc, int len, int splits, float* part, float* logits,
+                          int64_t lstride, hipStream_t st) {
+    if (D.dtype == 1) {
+        const int per = ((len + splits - 1) / splits + DEC_TILE - 1) / DEC_TILE * DEC_TILE;
+        LRSA_TIMED_LAUNCH("k_decode_mfma", st, (D.d == 64 ? k_decode_mfma<64, LOGITS> : k_decode_mfma<128, LOGITS>), dim3(splits, D.B * D.Hkv),
+                          dim3(DEC_THREADS), 0, st, D, (const bf16_t*)q, (const bf16_t*)Kc, (const bf16_t*)Vc, len, per, splits, part, logits,
+                          lstride);
+    } else {
+        LRSA_TIMED_LAUNCH("k_decode_attn", st, (k_decode_attn<float, LOGITS>), dim3(splits, D.B * D.Hkv), dim3(DEC_THREADS), 0, st, D,
+                          (const float*)q, (const float*)Kc, (const float*)Vc, len, splits, part, logits, lstride);
+    }
+}
+
 hipError_t launch_decode_attn(const Dims& D, const void* q, const void* Kc, const void* Vc, int len, void* O,
                               float* lse, void* ws, hipStream_t st) {
     const int splits = decode_splits(D, len);
     float* part = reinterpret_cast<float*>(ws);
-    if (D.dtype == 1) {
-        const int per = ((len + splits - 1) / splits + DEC_TILE - 1) / DEC_TILE * DEC_TILE;
-#define LRSA_DECODE_LAUNCH(DH_)                                                                                              \
-    LRSA_TIMED_LAUNCH("k_decode_mfma", st, k_decode_mfma<DH_>, dim3(splits, D.B * D.Hkv), dim3(DEC_THREADS), 0, st, D,       \
-                      (const bf16_t*)q, (const bf16_t*)Kc, (const bf16_t*)Vc, len, per, splits, part)
-        if (D.d == 64) LRSA_DECODE_LAUNCH(64); else LRSA_DECODE_LAUNCH(128);
-#undef LRSA_DECODE_LAUNCH
+    decode_slices<false>(D, q, Kc, Vc, len, splits, part, nullptr, 0, st);
+    if (D.dtype == 1)
         LRSA_TIMED_LAUNCH("k_decode_combine", st, k_decode_combine<bf16_t>, dim3(D.B * D.Hq), dim3(DEC_THREADS), 0, st, D, part, splits,
                           (bf16_t*)O, lse);
-    } else {
-        LRSA_TIMED_LAUNCH("k_decode_attn", st, k_decode_attn<float>, dim3(splits, D.B * D.Hkv), dim3(DEC_THREADS), 0, st, D,
-                          (const float*)q, (const float*)Kc, (const float*)Vc, len, splits, part);
+    else
         LRSA_TIMED_LAUNCH("k_decode_combine", st, k_decode_combine<float>, dim3(D.B * D.Hq), dim3(DEC_THREADS), 0, st, D, part, splits,
                           (float*)O, lse);
-    }
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------ with accumulated weights
+// A row's weights are known once every slice has been seen, so they need the logits a second time: stored in fp32, 8 bytes per
+// row and query head there and back, against 4 * d bytes of its key and value (a second read of K would be half of those).
+static int64_t logit_stride(int len) { return (int64_t(len) + DEC_TILE - 1) / DEC_TILE * DEC_TILE; }
+// the records' part, of the most slices that a cache of at most `len` rows is cut into: a workspace for a longer one is enough
+static size_t acc_part_bytes(const Dims& D, int len) {
+    const int a = decode_fine_splits(D, len), b = decode_static_splits(D, len);
+    return align256(part_bytes(D, a > b ? a : b));
+}
+size_t decode_acc_ws_bytes(const Dims& D, int len) {
+    return acc_part_bytes(D, len) + align256(size_t(D.B) * D.Hq * size_t(logit_stride(len)) * 4);
+}
+bool decode_acc_grid_fits(const Dims& D, int len) {
+    return grid_fits(int64_t(D.B) * D.Hq + int64_t(D.B) * D.Hkv * ((int64_t(len) + ACC_ROWS - 1) / ACC_ROWS), DEC_THREADS);
+}
+hipError_t launch_decode_attn_acc(const Dims& D, const void* q, const void* Kc, const void* Vc, int len, void* O, float* lse,
+                                  const float* acc_in, float* acc_out, float decay, void* ws, hipStream_t st) {
+    const int splits = decode_splits(D, len), chunks = (len - 1) / ACC_ROWS + 1;
+    float* part = reinterpret_cast<float*>(ws);
+    AccArgs A = {};
+    float* logits = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + acc_part_bytes(D, len));
+    A.logits = logits;
+    A.mul = D.scale * 1.4426950408889634f;
+    A.stride = logit_stride(len);
+    A.cols = D.G;
+    A.in = acc_in;
+    A.out = acc_out;
+    A.cap = D.n;
+    A.decay = decay;
+    decode_slices<true>(D, q, Kc, Vc, len, splits, part, logits, A.stride, st);
+    const dim3 grid(unsigned(D.B * D.Hq + D.B * D.Hkv * chunks));
+    if (D.dtype == 1)
+        LRSA_TIMED_LAUNCH("k_decode_combine_acc", st, k_decode_combine_acc<bf16_t>, grid, dim3(DEC_THREADS), 0, st, D, part, splits, (bf16_t*)O,
+                          lse, A, len, chunks);
+    else
+        LRSA_TIMED_LAUNCH("k_decode_combine_acc", st, k_decode_combine_acc<float>, grid, dim3(DEC_THREADS), 0, st, D, part, splits, (float*)O, lse,
+                          A, len, chunks);
     return hipGetLastError();
 }
 
