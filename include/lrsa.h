@@ -322,7 +322,7 @@ typedef enum { LRSA_QUANT_INT8 = 0, LRSA_QUANT_E4M3 = 1 /* OCP e4m3: no infiniti
 typedef struct {
     int32_t format;        /* lrsa_quant_format                                                                       */
     int32_t block;         /* rows per scale: 16, 32, 64 or 128                                                       */
-    int64_t stride[3];     /* BYTE strides of (batch, head, row) of K and V: row >= head_dim, all multiples of 16     */
+    int64_t stride[3];     /* BYTE strides of (batch, head, row) of K and V: head_dim <= row < 2^24, all multiples of 16 */
     void *K, *V;           /* codes [B, Hkv, cap, d_h] by stride, 16-byte aligned                                     */
     float *K_scale, *V_scale; /* [B, Hkv, ceil(cap / block)] contiguous                                               */
 } lrsa_quant_cache;

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -329,20 +330,55 @@ def lrsa_decode_attn_static(p: LrsaParams, q: torch.Tensor, Kc: torch.Tensor, Vc
 
 
 # ---- accumulated weights, eviction, the cache in 8 bits
-def _here(device: torch.device) -> None:
+# A single token's call takes the GPU 10 us, as long as the checks of its dozen tensors took on the host when they were written like those
+# above (lrsa_cache_evict 21.8 us a call).  So here the params are read in one go, and a tensor that fits is recognised by four
+# comparisons; only one that does not goes through _expect, which says why.
+_PARAMS = struct.Struct("@10if2i6q")
+
+
+def _read(p: LrsaParams):
+    """(batch, heads_q, heads_kv, seq, head_dim), torch dtype, (strides of K and V rows)"""
+    f = _PARAMS.unpack_from(p)
+    return f[:5], _TORCH_DTYPE.get(f[11]), f[16:19]
+
+
+def _here(t: torch.Tensor) -> int:
     """The library launches on the current device's current stream: tensors that live elsewhere are refused."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    i = t.get_device()
+    if i < 0 or i != torch.cuda.current_device():
+        raise ValueError(f"tensors on {t.device}, expected the current CUDA device")
+    return i
 
 
-def _call_ws(need: int, device, ws: Optional[torch.Tensor]) -> Tuple[Optional[torch.Tensor], int]:
+def _stream_of(index: int):
+    return _stream() if _raw_stream is None else _raw_stream(index)
+
+
+def _flat(name: str, t: Optional[torch.Tensor], shape, dtype, device) -> Optional[int]:
+    """The address of a contiguous tensor of that shape."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        _expect(name, t, shape, None, dtype, device)
+    return t.data_ptr()
+
+
+def _rows(name: str, t: Optional[torch.Tensor], shape, stride, dtype, device) -> Optional[int]:
+    """The address of a tensor of that shape and those strides."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.device != device or t.stride() != stride:
+        _expect(name, t, shape, stride, dtype, device)
+    return t.data_ptr()
+
+
+def _call_ws(need, device, ws: Optional[torch.Tensor]):
+    """Address and bytes of the caller's workspace, or of one for this call (then the tensor, too)."""
     if ws is None:
-        if need == 0:
-            return None, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws = torch.empty(need(), dtype=torch.uint8, device=device)
     elif ws.device != device or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {device}")
-    return ws, ws.numel() * ws.element_size()
+    return ws, ws.data_ptr(), ws.nbytes
 
 
 def decode_attn_acc_ws_bytes(p: LrsaParams, length: int) -> int:
@@ -354,21 +390,18 @@ def lrsa_decode_attn_acc(p: LrsaParams, q: torch.Tensor, Kc: torch.Tensor, Vc: t
                          ws: Optional[torch.Tensor] = None):
     """lrsa_decode_attn that also writes acc_out = decay * acc_in + the weight that every cache row received, summed over the heads of
     its group: acc [B, Hkv, cap] fp32, acc_in None for zeros, both may be the same tensor.  Returns (O, lse, acc_out)."""
-    dev, dt = q.device, _TORCH_DTYPE.get(p.dtype)
-    _here(dev)
+    index, dev, f32 = _here(q), q.device, torch.float32
+    (B, Hq, Hkv, cap, d), dt, ks = _read(p)
     if O is None:
-        O = torch.empty((p.batch, p.heads_q, p.head_dim), dtype=q.dtype, device=dev)
+        O = torch.empty((B, Hq, d), dtype=q.dtype, device=dev)
     if lse is None:
-        lse = torch.empty((p.batch, p.heads_q), dtype=torch.float32, device=dev)
-    for name, t in (("q", q), ("O", O)):
-        _expect(name, t, (p.batch, p.heads_q, p.head_dim), None, dt, dev)
-    _expect("lse", lse, (p.batch, p.heads_q), None, torch.float32, dev)
-    _expect_kv(p, dev, Kc=Kc, Vc=Vc)
-    for name, t in (("acc_in", acc_in), ("acc_out", acc_out)):
-        _expect(name, t, (p.batch, p.heads_kv, p.seq), None, torch.float32, dev)
-    ws, nb = _call_ws(decode_attn_acc_ws_bytes(p, length), dev, ws)
-    _check(lib().lrsa_decode_attn_acc(ctypes.byref(p), _ptr(q), _ptr(Kc), _ptr(Vc), int(length), _ptr(acc_in), _ptr(acc_out), float(decay),
-                                      _ptr(O), _ptr(lse), _ptr(ws), nb, _stream()))
+        lse = torch.empty((B, Hq), dtype=f32, device=dev)
+    one, kv, st, acc = (B, Hq, d), (B, Hkv, cap, d), (*ks, 1), (B, Hkv, cap)
+    args = (_flat("q", q, one, dt, dev), _rows("Kc", Kc, kv, st, dt, dev), _rows("Vc", Vc, kv, st, dt, dev), length,
+            _flat("acc_in", acc_in, acc, f32, dev), _flat("acc_out", acc_out, acc, f32, dev), decay, _flat("O", O, one, dt, dev),
+            _flat("lse", lse, (B, Hq), f32, dev))
+    ws, at, nb = _call_ws(lambda: decode_attn_acc_ws_bytes(p, length), dev, ws)
+    _check(lib().lrsa_decode_attn_acc(ctypes.byref(p), *args, at, nb, _stream_of(index)))
     return O, lse, acc_out
 
 
@@ -377,23 +410,19 @@ def cache_evict_ws_bytes(p: LrsaParams, length: int, budget: int) -> int:
     return int(lib().lrsa_cache_evict_ws_bytes(ctypes.byref(p), int(length), int(budget)))
 
 
-def _expect_lists(p: LrsaParams, dev, pos, acc, pos_o, acc_o) -> None:
-    for name, t, dt in (("pos", pos, torch.int32), ("acc", acc, torch.float32), ("pos_o", pos_o, torch.int32), ("acc_o", acc_o, torch.float32)):
-        _expect(name, t, (p.batch, p.heads_kv, p.seq), None, dt, dev)
-
-
 def lrsa_cache_evict(p: LrsaParams, Kc: torch.Tensor, Vc: torch.Tensor, pos: Optional[torch.Tensor], acc: torch.Tensor, length: int, budget: int,
                      recent: int, Ko: torch.Tensor, Vo: torch.Tensor, pos_o: Optional[torch.Tensor], acc_o: torch.Tensor,
                      ws: Optional[torch.Tensor] = None) -> int:
     """The first p.sink rows, the last `recent` and those of the others with the largest acc, `budget` in all, go to the cache Ko, Vo
     (with their positions and weights; weights behind them become zero).  Returns the new length."""
-    dev, new = Kc.device, ctypes.c_int32(0)
-    _here(dev)
-    _expect_kv(p, dev, Kc=Kc, Vc=Vc, Ko=Ko, Vo=Vo)
-    _expect_lists(p, dev, pos, acc, pos_o, acc_o)
-    ws, nb = _call_ws(cache_evict_ws_bytes(p, length, budget), dev, ws)
-    _check(lib().lrsa_cache_evict(ctypes.byref(p), _ptr(Kc), _ptr(Vc), _ptr(pos), _ptr(acc), int(length), int(budget), int(recent), _ptr(Ko),
-                                  _ptr(Vo), _ptr(pos_o), _ptr(acc_o), ctypes.byref(new), _ptr(ws), nb, _stream()))
+    index, dev, i32, f32 = _here(Kc), Kc.device, torch.int32, torch.float32
+    (B, _, Hkv, cap, d), dt, ks = _read(p)
+    kv, st, lst, new = (B, Hkv, cap, d), (*ks, 1), (B, Hkv, cap), ctypes.c_int32(0)
+    args = (_rows("Kc", Kc, kv, st, dt, dev), _rows("Vc", Vc, kv, st, dt, dev), _flat("pos", pos, lst, i32, dev), _flat("acc", acc, lst, f32, dev),
+            length, budget, recent, _rows("Ko", Ko, kv, st, dt, dev), _rows("Vo", Vo, kv, st, dt, dev), _flat("pos_o", pos_o, lst, i32, dev),
+            _flat("acc_o", acc_o, lst, f32, dev))
+    ws, at, nb = _call_ws(lambda: cache_evict_ws_bytes(p, length, budget), dev, ws)
+    _check(lib().lrsa_cache_evict(ctypes.byref(p), *args, ctypes.byref(new), at, nb, _stream_of(index)))
     return new.value
 
 
@@ -411,62 +440,57 @@ class QuantCache:
             raise ValueError("codes are [B, Hkv, cap, d] with a channel stride of 1")
         if block not in (16, 32, 64, 128):
             raise ValueError(f"blocks of {block} rows are not built (16, 32, 64 and 128 are)")
-        B, Hkv, cap, _ = K.shape
+        B, Hkv, cap, d = K.shape
         _expect("V", V, K.shape, K.stride(), K.dtype, K.device)
         for name, t in (("K_scale", K_scale), ("V_scale", V_scale)):
             _expect(name, t, (B, Hkv, -(-cap // block)), None, torch.float32, K.device)
-        self.K, self.V, self.K_scale, self.V_scale, self.block = K, V, K_scale, V_scale, block
+        self._tensors = K, V, K_scale, V_scale          # the struct holds their addresses: they are not exchanged
+        self.block, self.shape, self.device = block, (B, Hkv, cap, d), K.device
         # the stride of an axis of length 1 is whatever torch made it: any multiple of 16 serves
-        st = [s if n > 1 else K.shape[3] for s, n in zip(K.stride()[:3], K.shape[:3])]
-        self.struct = LrsaQuantCache(_QUANT_FORMATS[K.dtype], block, (ctypes.c_int64 * 3)(*st), K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr())
+        st = [s if n > 1 else d for s, n in zip(K.stride()[:3], K.shape[:3])]
+        self.struct = LrsaQuantCache(_QUANT_FORMATS[K.dtype], block, (ctypes.c_int64 * 3)(*st), *(t.data_ptr() for t in self._tensors))
         self.ref = ctypes.byref(self.struct)
+
+    K, V, K_scale, V_scale = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
     @classmethod
     def empty(cls, B: int, Hkv: int, cap: int, d: int, dtype=torch.int8, block: int = 64, device="cuda") -> "QuantCache":
         codes = [torch.zeros((B, Hkv, cap, d), dtype=torch.uint8, device=device).view(dtype) for _ in range(2)]
         return cls(*codes, *(torch.ones((B, Hkv, -(-cap // block)), dtype=torch.float32, device=device) for _ in range(2)), block)
 
-
-def _expect_cache(p: LrsaParams, name: str, c: QuantCache, device) -> None:
-    """The tensors were checked when the cache was made; here that it is the one that the params describe."""
-    if tuple(c.K.shape) != (p.batch, p.heads_kv, p.seq, p.head_dim):
-        raise ValueError(f"{name}: codes {tuple(c.K.shape)}, the params describe {(p.batch, p.heads_kv, p.seq, p.head_dim)}")
-    if c.K.device != device:
-        raise ValueError(f"{name}: on {c.K.device}, expected {device}")
-
-
-def _expect_new_rows(p: LrsaParams, device, rows: int, **tensors) -> None:
-    for name, t in tensors.items():
-        _expect(name, t, (p.batch, p.heads_kv, rows, p.head_dim), (*p.kv_stride, 1), _TORCH_DTYPE.get(p.dtype), device)
+    def _as(self, name: str, shape, device):
+        """The reference that the library takes, of a cache that the params describe (its tensors were checked when it was made)."""
+        if self.shape != shape:
+            raise ValueError(f"{name}: codes {self.shape}, the params describe {shape}")
+        if self.device != device:
+            raise ValueError(f"{name}: on {self.device}, expected {device}")
+        return self.ref
 
 
 def lrsa_cache_append_quant(p: LrsaParams, cache: QuantCache, K: torch.Tensor, V: torch.Tensor, lens: torch.Tensor,
                             counts: Optional[torch.Tensor] = None) -> None:
     """Rows lens[b] .. of the cache become the first counts[b] (None: all) rows of K and V [B, Hkv, tokens, d], strides as p.kv_stride says;
     lens, counts: [B] int32 on the device, not changed."""
-    dev = K.device
-    _here(dev)
-    _expect_cache(p, "cache", cache, dev)
+    index, dev, i32 = _here(K), K.device, torch.int32
+    (B, _, Hkv, cap, d), dt, ks = _read(p)
     tokens = K.shape[2]
-    _expect_new_rows(p, dev, tokens, K=K, V=V)
-    for name, t in (("lens", lens), ("counts", counts)):
-        _expect(name, t, (p.batch,), None, torch.int32, dev)
-    _check(lib().lrsa_cache_append_quant(ctypes.byref(p), cache.ref, _ptr(K), _ptr(V), tokens, _ptr(lens), _ptr(counts), _stream()))
+    kv, st = (B, Hkv, tokens, d), (*ks, 1)
+    _check(lib().lrsa_cache_append_quant(ctypes.byref(p), cache._as("cache", (B, Hkv, cap, d), dev), _rows("K", K, kv, st, dt, dev),
+                                         _rows("V", V, kv, st, dt, dev), tokens, _flat("lens", lens, (B,), i32, dev),
+                                         _flat("counts", counts, (B,), i32, dev), _stream_of(index)))
 
 
 def lrsa_cache_read_quant(p: LrsaParams, cache: QuantCache, lens: torch.Tensor, rows: int, first: Optional[torch.Tensor] = None,
                           K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
     """Rows first[b] (None: 0) .. + rows of every sequence as values [B, Hkv, rows, d], zero at and behind lens[b]; returns (K, V), by
     default of the strides that p.kv_stride gives."""
-    dev, dt = cache.K.device, _TORCH_DTYPE.get(p.dtype)
-    _here(dev)
-    _expect_cache(p, "cache", cache, dev)
-    rows = int(rows)
-    K, V = (torch.empty_strided((p.batch, p.heads_kv, rows, p.head_dim), (*p.kv_stride, 1), dtype=dt, device=dev) if t is None else t for t in (K, V))
-    _expect_new_rows(p, dev, rows, K=K, V=V)
-    for name, t in (("lens", lens), ("first", first)):
-        _expect(name, t, (p.batch,), None, torch.int32, dev)
-    _check(lib().lrsa_cache_read_quant(ctypes.byref(p), cache.ref, _ptr(lens), rows, _ptr(first), _ptr(K), _ptr(V), _stream()))
+    index, dev, i32 = _here(lens), lens.device, torch.int32
+    (B, _, Hkv, cap, d), dt, ks = _read(p)
+    kv, st = (B, Hkv, rows, d), (*ks, 1)
+    K, V = (torch.empty_strided(kv, st, dtype=dt, device=dev) if t is None else t for t in (K, V))
+    _check(lib().lrsa_cache_read_quant(ctypes.byref(p), cache._as("cache", (B, Hkv, cap, d), dev), _flat("lens", lens, (B,), i32, dev), rows,
+                                       _flat("first", first, (B,), i32, dev), _rows("K", K, kv, st, dt, dev), _rows("V", V, kv, st, dt, dev),
+                                       _stream_of(index)))
     return K, V
 
 
@@ -480,24 +504,20 @@ def lrsa_decode_attn_quant(p: LrsaParams, q: torch.Tensor, cache: QuantCache, le
     """Attention of the last tokens of every sequence over the cache: q, O [B, Hq, tokens, d] (or [B, Hq, d]: one token), lens [B] int32 on
     the device, none above max_len; token t sees the rows below lens[b] - tokens + 1 + t.  With acc_out, the rows' weights are added up
     as in lrsa_decode_attn_acc.  Returns (O, lse [B, Hq, tokens] fp32)."""
-    dev, dt = q.device, _TORCH_DTYPE.get(p.dtype)
-    _here(dev)
-    _expect_cache(p, "cache", cache, dev)
+    index, dev, f32 = _here(q), q.device, torch.float32
+    (B, Hq, Hkv, cap, d), dt, _ = _read(p)
     tokens = q.shape[2] if q.dim() == 4 else 1
-    shape = (p.batch, p.heads_q, tokens, p.head_dim) if q.dim() == 4 else (p.batch, p.heads_q, p.head_dim)
+    rows = (B, Hq, tokens) if q.dim() == 4 else (B, Hq)
+    shape, acc = (*rows, d), (B, Hkv, cap)
     if O is None:
         O = torch.empty(shape, dtype=q.dtype, device=dev)
     if lse is None:
-        lse = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
-    for name, t in (("q", q), ("O", O)):
-        _expect(name, t, shape, None, dt, dev)
-    _expect("lse", lse, shape[:-1], None, torch.float32, dev)
-    _expect("lens", lens, (p.batch,), None, torch.int32, dev)
-    for name, t in (("acc_in", acc_in), ("acc_out", acc_out)):
-        _expect(name, t, (p.batch, p.heads_kv, p.seq), None, torch.float32, dev)
-    ws, nb = _call_ws(decode_attn_quant_ws_bytes(p, tokens, max_len, acc_out is not None), dev, ws)
-    _check(lib().lrsa_decode_attn_quant(ctypes.byref(p), cache.ref, _ptr(q), tokens, _ptr(lens), int(max_len), _ptr(acc_in), _ptr(acc_out),
-                                        float(decay), _ptr(O), _ptr(lse), _ptr(ws), nb, _stream()))
+        lse = torch.empty(rows, dtype=f32, device=dev)
+    args = (cache._as("cache", (B, Hkv, cap, d), dev), _flat("q", q, shape, dt, dev), tokens, _flat("lens", lens, (B,), torch.int32, dev), max_len,
+            _flat("acc_in", acc_in, acc, f32, dev), _flat("acc_out", acc_out, acc, f32, dev), decay, _flat("O", O, shape, dt, dev),
+            _flat("lse", lse, rows, f32, dev))
+    ws, at, nb = _call_ws(lambda: decode_attn_quant_ws_bytes(p, tokens, max_len, acc_out is not None), dev, ws)
+    _check(lib().lrsa_decode_attn_quant(ctypes.byref(p), *args, at, nb, _stream_of(index)))
     return O, lse
 
 
@@ -505,16 +525,14 @@ def lrsa_cache_evict_quant(p: LrsaParams, cache: QuantCache, pos: Optional[torch
                            budget: int, recent: int, out: QuantCache, pos_o: Optional[torch.Tensor], acc_o: torch.Tensor, lens_o: torch.Tensor,
                            ws: Optional[torch.Tensor] = None) -> None:
     """lrsa_cache_evict from one cache in 8 bits to another of the same format and block; lens -> lens_o, [B] int32 on the device."""
-    dev = acc.device
-    _here(dev)
-    _expect_cache(p, "cache", cache, dev)
-    _expect_cache(p, "out", out, dev)
-    _expect_lists(p, dev, pos, acc, pos_o, acc_o)
-    for name, t in (("lens", lens), ("lens_o", lens_o)):
-        _expect(name, t, (p.batch,), None, torch.int32, dev)
-    ws, nb = _call_ws(cache_evict_ws_bytes(p, max_len, budget), dev, ws)
-    _check(lib().lrsa_cache_evict_quant(ctypes.byref(p), cache.ref, _ptr(pos), _ptr(acc), _ptr(lens), int(max_len), int(budget), int(recent),
-                                        out.ref, _ptr(pos_o), _ptr(acc_o), _ptr(lens_o), _ptr(ws), nb, _stream()))
+    index, dev, i32, f32 = _here(acc), acc.device, torch.int32, torch.float32
+    (B, _, Hkv, cap, d), _, _ = _read(p)
+    kv, lst = (B, Hkv, cap, d), (B, Hkv, cap)
+    args = (cache._as("cache", kv, dev), _flat("pos", pos, lst, i32, dev), _flat("acc", acc, lst, f32, dev), _flat("lens", lens, (B,), i32, dev), max_len,
+            budget, recent, out._as("out", kv, dev), _flat("pos_o", pos_o, lst, i32, dev), _flat("acc_o", acc_o, lst, f32, dev),
+            _flat("lens_o", lens_o, (B,), i32, dev))
+    ws, at, nb = _call_ws(lambda: cache_evict_ws_bytes(p, max_len, budget), dev, ws)
+    _check(lib().lrsa_cache_evict_quant(ctypes.byref(p), *args, at, nb, _stream_of(index)))
 
 
 def lrsa_attn_fwd(p: LrsaParams, Q, K, V, idx, O: Optional[torch.Tensor] = None,

@@ -494,6 +494,7 @@ int make_quant(const char* who, const lrsa::Dims& D, const lrsa_quant_cache* c, 
     for (int i = 0; i < 3; ++i)
         if (c->stride[i] < 0 || c->stride[i] % 16 != 0)
             return fail(LRSA_ERR_INVALID_ARG, "%s: stride %lld of the codes is negative or no multiple of 16", who, (long long)c->stride[i]);
+    if (c->stride[2] >= (int64_t)1 << 24) return fail(LRSA_ERR_UNSUPPORTED, "%s: rows %lld bytes apart (2^24 and more are not built)", who, (long long)c->stride[2]);
     Q->fmt = c->format == LRSA_QUANT_INT8 ? lrsa::QUANT_INT8 : lrsa::QUANT_E4M3;
     Q->block = c->block;
     Q->log_block = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;

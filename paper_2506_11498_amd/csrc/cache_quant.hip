@@ -91,24 +91,78 @@ __global__ __launch_bounds__(QUANT_THREADS) void k_read_quant(Dims D, QuantDims 
 }
 
 // ------------------------------------------------------------------------------------ attention
-// One workgroup: the query rows of one KV group (16 at a time) x rows [split * per, ...) of the cache, as k_decode_mfma.  A
-// query row ("column") is (head of the group, token): q is [B, Hq, T, d], so the columns of a unit are neighbours.  Lane l, c =
-// l % 16, q4 = l / 16, v_mfma_f32_16x16x32_bf16:
-//   S = K Q^T   row m of block kb is tile row 8*(m/4) + 4*kb + m%4.  The contraction over the channels may take them in any
-//               order: the lane reads 16 neighbouring bytes (channels 64*i + 16*q4 ..), two instructions' worth
-//   O^T += V^T P^T   the lane reads DH/16 neighbouring channels of tile rows 8*q4 .. +7 and transposes that block
+// How the rows are cut into slices, W workgroups being what runs at once.
+//   even  Where all sequences of max_len rows give no more than W slices of 4 tiles, a slice has that length: workgroup
+//         (b * Hkv + h) * splits + s takes slice s, and exits where the sequence is shorter.
+//   else  The sequences' lengths are known on the device only, so every workgroup takes them from there: with t_b tiles in
+//         sequence b, a slice is sum(t_b) * Hkv / W tiles if that gives W slices at most (the last of a sequence is short), or
+//         sum(t_b) * Hkv / (W - B * Hkv), which always does (estimates in floating point that are never too small).  Slices of
+//         equal length then begin and end together however the lengths are mixed: 8 requests of 11K to 32K rows, 8 KV heads, 78 us,
+//         with slices by max_len 88.  Slice s of KV head h of sequence b is workgroup Hkv * (slices of the sequences before) + h *
+//         n_b + s.
+constexpr int QT = 32;                       // rows of a tile: per wave and step
+struct QuantSlices {
+    int splits;                              // even: slices per unit, else 0
+    int most, least;                         // W; the least tiles of a slice
+    float share, safe;                       // Hkv / W, Hkv / (W - B * Hkv), rounded up
+};
+struct QuantSeq { int base, n; };            // of one sequence: workgroup of its first slice, slices per KV head
+
+// wave-wide; `each` gets the tiles of the sequences in groups of 64, one per lane, until it returns true
+template <class Fn>
+__device__ __forceinline__ void each_sequence(const Dims& D, const int32_t* lens, int max_len, Fn each) {
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < D.B; b0 += 64) {
+        const int b = b0 + lane;
+        if (each(b, b < D.B ? (seq_len(lens, b, max_len) + QT - 1) / QT : 0)) return;
+    }
+}
+__device__ __forceinline__ int tiles_sum(int v) { return __builtin_amdgcn_readlane(wave_iscan(v), 63); }
+__device__ __forceinline__ int slice_tiles(const Dims& D, const int32_t* lens, int max_len, const QuantSlices& S) {
+    int sum = 0, count = 0;
+    each_sequence(D, lens, max_len, [&](int, int t) { sum += t; return false; });
+    const float all = float(tiles_sum(sum));
+    const int per = max(int(all * S.share) + 1, S.least);
+    each_sequence(D, lens, max_len, [&](int, int t) { count += (t + per - 1) / per; return false; });
+    return __builtin_amdgcn_readfirstlane(int64_t(tiles_sum(count)) * D.Hkv <= S.most ? per : max(int(all * S.safe) + 1, S.least));
+}
+
+// One workgroup: the query rows of one KV group x a slice of the cache rows, as k_decode_mfma.  A query row ("column") is
+// (head of the group, token): q is [B, Hq, T, d], so the columns of a unit are neighbours.  Lane l, c = l % 16, q4 = l / 16,
+// v_mfma_f32_16x16x32_bf16:
+//   S = K Q^T   row m of block kb is tile row 16*kb + m.  The contraction over the channels may take them in any order: the
+//               lane reads 16 neighbouring bytes (channels 64*i + 16*q4 ..), two instructions' worth.  It then holds the
+//               logits of rows 4*q4 .. +3 and 16 + 4*q4 .. +3 of column c, which are the k-slots of its B operand below
+//   O^T += V^T P^T   the lane reads DH/16 neighbouring channels of those rows and transposes that block
 // Codes have at most 8 significant bits, so both operands are exact in bf16 without their scales; the scale of K multiplies
-// the logit, that of V the weight, in fp32 (8 neighbouring rows of a tile share a block: blocks are multiples of 16).  Queries
-// of fp32 enter as three bf16 terms, which hold all 24 bits, and so do the weights.
-constexpr int QT = 32;                       // rows per wave and step
+// the logit, that of V the weight, in fp32 (4 such rows share a block: blocks are multiples of 16).  Queries of fp32 enter as
+// three bf16 terms, which hold all 24 bits, and so do the weights.
+// Up to 16 columns: the 4 waves take the tiles in turn (SOLE), every code is read by one wave of the chip, past the caches.
+// More: `groups` (2 or 4) waves take the same tile, 16 columns each, so that its codes come from memory once; beyond 64
+// columns the slice is walked again.
+// The next tile's loads are in flight while a tile is used.  They are issued in every turn (the last one asks for its own tile
+// again, from the caches): loads in a branch make the compiler wait for all of them at its end, the next tile's too.
 constexpr float NO_WEIGHT = -1e30f;          // running maximum before the first visible row: finite, so that differences are
-template <int DH> struct QPiece { typedef uint2 type; };
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int DH> struct QPiece { typedef u32x2 type; };
 template <> struct QPiece<64> { typedef uint32_t type; };
 template <int DH> struct QuantTile {
-    uint4 k[2][DH / 64];
+    u32x4 k[2][DH / 64];
     typename QPiece<DH>::type v[8];
-    float ks, vs;
+    float ks[2], vs[2];
 };
+struct QuantRows {                           // of one unit
+    const uint8_t *K, *V;
+    const float *Ks, *Vs;
+    int64_t st;
+    int log_block;
+};
+template <bool SOLE, typename V>
+__device__ __forceinline__ V load_codes(const uint8_t* p) {
+    if constexpr (SOLE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    return *reinterpret_cast<const V*>(p);
+}
 
 // 4 codes -> two bf16 pairs
 template <int FMT>
@@ -122,51 +176,74 @@ __device__ __forceinline__ void codes_bf16(uint32_t w, uint32_t& lo, uint32_t& h
         hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
     }
 }
-
-template <int DH>
-__device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantDims& Q, const uint8_t* Kl, const uint8_t* Vl, const float* Ks,
-                                                const float* Vs, int kr, int vr, int last) {
+// 4 codes of a row and the 4 below them -> for each of the 4 columns a bf16 pair (upper row first)
+template <int FMT>
+__device__ __forceinline__ void codes_bf16_columns(uint32_t w0, uint32_t w1, uint32_t (&col)[4]) {
+    if constexpr (FMT == QUANT_INT8) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-        const uint8_t* row = Kl + int64_t(min(kr + 4 * kb, last)) * Q.st[2];   // rows past the end repeat the last one, weight 0
-#pragma unroll
-        for (int i = 0; i < DH / 64; ++i) t.k[kb][i] = *reinterpret_cast<const uint4*>(row + i * 64);
+        for (int i = 0; i < 4; ++i)
+            col[i] = __builtin_amdgcn_perm(__float_as_uint(float(int8_t(w1 >> (8 * i)))), __float_as_uint(float(int8_t(w0 >> (8 * i)))), 0x07060302u);
+    } else {
+        const uint32_t lo = __builtin_amdgcn_perm(w1, w0, 0x05010400u), hi = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
+        codes_bf16<FMT>(lo, col[0], col[1]);
+        codes_bf16<FMT>(hi, col[2], col[3]);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) t.v[j] = *reinterpret_cast<const typename QPiece<DH>::type*>(Vl + int64_t(min(vr + j, last)) * Q.st[2]);
-    const int block = min(vr, last) >> Q.log_block;
-    t.ks = Ks[block];
-    t.vs = Vs[block];
 }
 
-// r: the first of the lane's rows; seen: rows from there on that its column sees
-template <int DH, int FMT, int TERMS>
+// r: the tile's first row (wave-uniform), of rows up to `last`: rows past the end repeat it, their weight will be 0
+template <int DH, bool SOLE>
+__device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantRows& R, int r, int q4, int c, int last) {
+    const uint8_t *K = R.K + r * R.st, *V = R.V + r * R.st;
+    const uint32_t most = min(last - r, QT - 1), st = uint32_t(R.st);        // rows are less than 2^24 bytes apart
+    auto off = [&](uint32_t row) { return __umul24(min(row, most), st); };
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t row = off(16 * kb + c) + q4 * 16;
+#pragma unroll
+        for (int i = 0; i < DH / 64; ++i) t.k[kb][i] = load_codes<SOLE, u32x4>(K + row + i * 64);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t.v[j] = load_codes<SOLE, typename QPiece<DH>::type>(V + (off(4 * q4 + j % 4 + j / 4 * 16) + c * (DH / 16)));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t block = (r + min(uint32_t(16 * i + 4 * q4), most)) >> R.log_block;
+        t.ks[i] = R.Ks[block];
+        t.vs[i] = R.Vs[block];
+    }
+}
+
+// Keeps the compiler from taking codes apart before their tile is used: a tile of int8 as floats, ready for the loop's next turn,
+// takes 128 registers instead of 32 (and spilled).
+__device__ __forceinline__ uint32_t as_loaded(uint32_t w) {
+    asm("" : "+v"(w));
+    return w;
+}
+
+// seen: rows from the lane's first one on that its column sees; ACC: the logits go to `out`
+template <int DH, int FMT, int TERMS, bool ACC>
 __device__ __forceinline__ void use_quant_tile(float& m, float& l, f32x4 (&o)[DH / 16], const QuantTile<DH>& t, const bf16x8 (&qf)[TERMS][DH / 32],
-                                               int seen, float c2, float* logits) {
+                                               int seen, float c2, LogitBuffer& out) {
     f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kk = 0; kk < DH / 32; ++kk)
 #pragma unroll
-        for (int kk = 0; kk < DH / 32; ++kk) {
-            const uint4 w = t.k[kb][kk / 2];
+        for (int kb = 0; kb < 2; ++kb) {
+            const u32x4 w = t.k[kb][kk / 2];
             uint32_t a[4];
-            codes_bf16<FMT>(kk % 2 ? w.z : w.x, a[0], a[1]);
-            codes_bf16<FMT>(kk % 2 ? w.w : w.y, a[2], a[3]);
+            codes_bf16<FMT>(as_loaded(kk % 2 ? w.z : w.x), a[0], a[1]);
+            codes_bf16<FMT>(as_loaded(kk % 2 ? w.w : w.y), a[2], a[3]);
             const bf16x8 kf = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
             for (int i = TERMS - 1; i >= 0; --i) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][kk], s[kb], 0, 0, 0);
         }
     float p[8], mx = NO_WEIGHT;
-    const float c2s = c2 * t.ks;
+    const float c2s[2] = {c2 * t.ks[0], c2 * t.ks[1]};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        p[j] = j < seen ? s[j >> 2][j & 3] * c2s : -INFINITY;
+        p[j] = j % 4 + j / 4 * 16 < seen ? s[j >> 2][j & 3] * c2s[j >> 2] : -INFINITY;
         mx = fmaxf(mx, p[j]);
     }
-    if (logits) {
-        reinterpret_cast<f32x4*>(logits)[0] = f32x4{p[0], p[1], p[2], p[3]};
-        reinterpret_cast<f32x4*>(logits)[1] = f32x4{p[4], p[5], p[6], p[7]};
-    }
+    if constexpr (ACC) keep_logits(out, p, [](int j) { return 4 * int(threadIdx.x >> 4 & 3) + j % 4 + j / 4 * 16; });
     lanes_u32x2 x = pair32(__float_as_uint(mx));
     mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
     x = pair16(__float_as_uint(mx));
@@ -184,7 +261,7 @@ __device__ __forceinline__ void use_quant_tile(float& m, float& l, f32x4 (&o)[DH
     for (int j = 0; j < 8; ++j) {
         const float e = __builtin_amdgcn_exp2f(p[j] - m);
         ps += e;
-        w[j] = e * t.vs;
+        w[j] = e * t.vs[j >> 2];
     }
     l += ps;
     bf16x8 term[3];
@@ -193,20 +270,20 @@ __device__ __forceinline__ void use_quant_tile(float& m, float& l, f32x4 (&o)[DH
         term[i] = __builtin_convertvector(w, bf16x8);
         w -= __builtin_convertvector(term[i], f32x8);
     }
-    constexpr int DW = DH / 64;              // dwords of codes per row
-    uint32_t b[8][2 * DW];                   // the same as bf16 pairs
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int e0 = 0; e0 < DH / 16; e0 += 4) {
+        uint32_t col[4][4];                  // [pair of rows][column]
 #pragma unroll
-        for (int i = 0; i < DW; ++i) codes_bf16<FMT>(reinterpret_cast<const uint32_t*>(&t.v[j])[i], b[j][2 * i], b[j][2 * i + 1]);
+        for (int i = 0; i < 4; ++i)
+            codes_bf16_columns<FMT>(as_loaded(reinterpret_cast<const uint32_t*>(&t.v[2 * i])[e0 / 4]),
+                                    as_loaded(reinterpret_cast<const uint32_t*>(&t.v[2 * i + 1])[e0 / 4]), col[i]);
 #pragma unroll
-    for (int e = 0; e < DH / 16; ++e) {
-        uint32_t a[4];
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t a[4] = {col[0][e], col[1][e], col[2][e], col[3][e]};
+            const bf16x8 av = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(b[2 * i + 1][e >> 1], b[2 * i][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-        const bf16x8 av = __builtin_bit_cast(bf16x8, a);
-#pragma unroll
-        for (int i = 2; i >= 0; --i) o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, term[i], o[e], 0, 0, 0);
+            for (int i = 2; i >= 0; --i) o[e0 + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, term[i], o[e0 + e], 0, 0, 0);
+        }
     }
 }
 
@@ -227,56 +304,90 @@ __device__ __forceinline__ void query_terms(const float* q, bf16x8 (&f)[3]) {
 
 template <typename T> constexpr int Q_TERMS = sizeof(T) == 2 ? 1 : 3;
 
-template <typename T, int DH, int FMT>
+template <typename T, int DH, int FMT, bool SOLE, bool ACC>
 __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDims Q, const T* __restrict__ q, int tokens, const int32_t* __restrict__ lens,
-                                                                 int max_len, int per, int splits, float* __restrict__ part,
-                                                                 float* __restrict__ logits, int64_t lstride) {
-    constexpr int CPL = DH / 16, LROW = DH + 4, TERMS = Q_TERMS<T>;
-    __shared__ __attribute__((aligned(16))) float sO[DEC_WAVES][16][LROW];
+                                                                 int max_len, QuantSlices S, QuantSeq* __restrict__ seqs, float* __restrict__ part,
+                                                                 float* __restrict__ logits, int64_t lrows, int pitch) {
+    constexpr int CPL = DH / 16, LROW = DH + 4, TERMS = Q_TERMS<T>, REC = DH + 2;
+    constexpr int WAVE_FLOATS = ACC ? LOGIT_FLOATS : 16 * LROW;      // a wave's logits, then its output
+    static_assert(WAVE_FLOATS >= 16 * LROW, "LDS of a wave");
+    __shared__ __attribute__((aligned(16))) float sBuf[DEC_WAVES][WAVE_FLOATS];
     __shared__ float sM[DEC_WAVES][16], sL[DEC_WAVES][16];
-    const int split = blockIdx.x, bh = blockIdx.y, b = bh / D.Hkv, h = bh % D.Hkv;
-    const int len = seq_len(lens, b, max_len);
-    const int r0 = split * per, r1 = min(len, r0 + per);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q4 = lane >> 4;
+    const int wg = blockIdx.x;
+    int b = -1, h, r0, per;
+    if (S.splits) {
+        const int unit = wg / S.splits;
+        b = unit / D.Hkv;
+        h = unit % D.Hkv;
+        per = S.least;
+        r0 = wg % S.splits * per * QT;
+    } else {
+        // the sequence of this workgroup; the first workgroup notes all of them for the merge
+        int first = 0, n = 1, before = 0;
+        per = slice_tiles(D, lens, max_len, S);
+        each_sequence(D, lens, max_len, [&](int bb, int t) {
+            const int mine = (t + per - 1) / per, upto = before + D.Hkv * wave_iscan(mine);
+            if (wg == 0 && wave == 0 && bb < D.B) seqs[bb] = QuantSeq{upto - D.Hkv * mine, mine};
+            const uint64_t at = __builtin_amdgcn_ballot_w64(wg >= upto - D.Hkv * mine && wg < upto);
+            if (at != 0 && b < 0) {
+                const int l = __builtin_ctzll(at);
+                b = (bb - lane) + l;
+                n = __builtin_amdgcn_readlane(mine, l);
+                first = __builtin_amdgcn_readlane(upto, l) - D.Hkv * n;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+            return b >= 0 && wg != 0;
+        });
+        if (b < 0) return;
+        b = __builtin_amdgcn_readfirstlane(b);
+        h = (wg - first) / n;
+        r0 = (wg - first) % n * per * QT;
+    }
+    const int bh = b * D.Hkv + h, len = seq_len(lens, b, max_len), r1 = min(len, r0 + per * QT);
     if (r0 >= r1) return;                                    // an empty slice: the merge does not ask for it
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, q4 = lane >> 4;
-    const uint8_t* Kl = Q.K + b * Q.st[0] + h * Q.st[1] + q4 * 16;
-    const uint8_t* Vl = Q.V + b * Q.st[0] + h * Q.st[1] + c * CPL;
-    const float *Ks = Q.Ks + int64_t(bh) * Q.nb, *Vs = Q.Vs + int64_t(bh) * Q.nb;
-    const int kr = 8 * (c >> 2) + (c & 3), vr = 8 * q4;
+    const int64_t head = b * Q.st[0] + h * Q.st[1];
+    const QuantRows R = {Q.K + head, Q.V + head, Q.Ks + int64_t(bh) * Q.nb, Q.Vs + int64_t(bh) * Q.nb, Q.st[2], Q.log_block};
     const float c2 = D.scale * 1.4426950408889634f;          // logits in log2 units
-    const int cols = D.G * tokens;
+    const int cols = D.G * tokens, groups = SOLE ? 1 : cols <= 32 ? 2 : 4, ways = DEC_WAVES / groups;
     const int64_t col0 = int64_t(bh) * cols;                 // query rows of the units before
 
-    for (int g0 = 0; g0 < cols; g0 += 16) {
-        const int gn = min(16, cols - g0), col = g0 + min(c, gn - 1);
-        const int vis = len - tokens + 1 + col % tokens;     // rows that the column sees, none where that is not positive
-        const T* qrow = q + (col0 + col) * DH;
-        bf16x8 qf[TERMS][DH / 32];
-#pragma unroll
-        for (int kk = 0; kk < DH / 32; ++kk) {
-            bf16x8 f[TERMS];
-            query_terms(qrow + (kk / 2) * 64 + q4 * 16 + (kk % 2) * 8, f);
-#pragma unroll
-            for (int i = 0; i < TERMS; ++i) qf[i][kk] = f[i];
-        }
+    for (int c0 = 0; c0 < cols; c0 += 16 * groups) {
+        const int g0 = c0 + 16 * (wave % groups), gn = min(16, cols - g0);      // of this wave: none where not positive
         float m = NO_WEIGHT, l = 0.0f;
         f32x4 o[CPL];
 #pragma unroll
         for (int e = 0; e < CPL; ++e) o[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        constexpr int STEP = DEC_WAVES * QT;
-        float* lrow = logits && c < gn ? logits + (col0 + g0 + c) * lstride + vr : nullptr;
-        int r = r0 + wave * QT;
-        if (r < r1) {
+        const int step = ways * QT;
+        int r = r0 + wave / groups * QT;
+        if (gn > 0 && r < r1) {
+            const int col = g0 + min(c, gn - 1);
+            const int vis = len - tokens + 1 + col % tokens;     // rows that the column sees, none where that is not positive
+            const T* qrow = q + (col0 + col) * DH;
+            const int end = r + (r1 - 1 - r) / step * step;      // the wave's last tile
+            auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, SOLE>(t, R, min(row, end), q4, c, r1 - 1); };
             QuantTile<DH> A, B;
-            load_quant_tile<DH>(A, Q, Kl, Vl, Ks, Vs, r + kr, r + vr, r1 - 1);
-            for (;;) {
-                if (r + STEP < r1) load_quant_tile<DH>(B, Q, Kl, Vl, Ks, Vs, r + STEP + kr, r + STEP + vr, r1 - 1);
-                use_quant_tile<DH, FMT, TERMS>(m, l, o, A, qf, min(r1, vis) - r - vr, c2, lrow ? lrow + r : nullptr);
-                if ((r += STEP) >= r1) break;
-                if (r + STEP < r1) load_quant_tile<DH>(A, Q, Kl, Vl, Ks, Vs, r + STEP + kr, r + STEP + vr, r1 - 1);
-                use_quant_tile<DH, FMT, TERMS>(m, l, o, B, qf, min(r1, vis) - r - vr, c2, lrow ? lrow + r : nullptr);
-                if ((r += STEP) >= r1) break;
+            load(A, r);
+            bf16x8 qf[TERMS][DH / 32];
+#pragma unroll
+            for (int kk = 0; kk < DH / 32; ++kk) {
+                bf16x8 f[TERMS];
+                query_terms(qrow + (kk / 2) * 64 + q4 * 16 + (kk % 2) * 8, f);
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) qf[i][kk] = f[i];
             }
+            LogitBuffer out = {};
+            if constexpr (ACC) out = logit_buffer(sBuf[wave], logits + (int64_t(bh) * lrows + r) * pitch + g0, pitch, gn, step);
+            auto use = [&](const QuantTile<DH>& t) { use_quant_tile<DH, FMT, TERMS, ACC>(m, l, o, t, qf, min(r1, vis) - r - 4 * q4, c2, out); };
+            for (;;) {
+                load(B, r + step);
+                use(A);
+                if ((r += step) >= r1) break;
+                load(A, r + step);
+                use(B);
+                if ((r += step) >= r1) break;
+            }
+            if constexpr (ACC) flush_logits(out);
         }
         lanes_u32x2 x = pair32(__float_as_uint(l));
         l = __uint_as_float(x.x) + __uint_as_float(x.y);
@@ -288,19 +399,19 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < CPL; e += 4)
-                    *reinterpret_cast<f32x4*>(&sO[wave][c][(4 * q4 + i) * CPL + e]) = f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
+                    *reinterpret_cast<f32x4*>(&sBuf[wave][c * LROW + (4 * q4 + i) * CPL + e]) = f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
         }
         __syncthreads();
-        for (int e = tid; e < gn * DH; e += DEC_THREADS) {
-            const int g = e / DH, ch = e % DH;
-            float mm = sM[0][g], ll = sL[0][g], oo = sO[0][g][ch];
-#pragma unroll
-            for (int w = 1; w < DEC_WAVES; ++w) {
+        // column g of the walk is in the waves g / 16, + groups, ...
+        for (int e = tid; e < min(16 * groups, cols - c0) * DH; e += DEC_THREADS) {
+            const int g = e / DH, ch = e % DH, w0 = g >> 4, gc = g & 15;
+            float mm = sM[w0][gc], ll = sL[w0][gc], oo = sBuf[w0][gc * LROW + ch];
+            for (int w = w0 + groups; w < DEC_WAVES; w += groups) {
                 float a, b2;
-                merge_state(mm, ll, sM[w][g], sL[w][g], a, b2);
-                oo = oo * a + sO[w][g][ch] * b2;
+                merge_state(mm, ll, sM[w][gc], sL[w][gc], a, b2);
+                oo = oo * a + sBuf[w][gc * LROW + ch] * b2;
             }
-            float* dst = part + ((col0 + g0 + g) * splits + split) * (DH + 2);
+            float* dst = part + (int64_t(wg) * cols + c0 + g) * REC;
             dst[2 + ch] = oo;
             if (ch == 0) { dst[0] = mm; dst[1] = ll; }
         }
@@ -310,22 +421,35 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
 
 // The first `rows` workgroups merge the slices of a query row each; the others, where weights are accumulated, take ACC_ROWS
 // cache rows of a unit each.
+__device__ __forceinline__ void unit_slices(const Dims& D, const QuantSlices& S, const QuantSeq* seqs, int unit, int len, int& base, int& n) {
+    if (S.splits) {
+        base = unit * S.splits;
+        n = (len + S.least * QT - 1) / (S.least * QT);
+    } else {
+        const QuantSeq s = seqs[unit / D.Hkv];
+        base = s.base + unit % D.Hkv * s.n;
+        n = s.n;
+    }
+}
 template <typename T>
 __global__ __launch_bounds__(DEC_THREADS) void k_quant_combine(Dims D, const float* __restrict__ part, int tokens, const int32_t* __restrict__ lens,
-                                                               int max_len, int per, int splits, T* __restrict__ O, float* __restrict__ lse,
-                                                               AccArgs A, int rows, int chunks) {
+                                                               int max_len, QuantSlices S, const QuantSeq* __restrict__ seqs, T* __restrict__ O,
+                                                               float* __restrict__ lse, AccArgs A, int rows, int chunks) {
     __shared__ union { CombineLds c; float lse[ACC_COLS]; } sh;
     const int rec = D.d + 2, cols = D.G * tokens;
+    const int64_t step = int64_t(cols) * rec;
+    int base, n;
     if (int(blockIdx.x) < rows) {
-        const int64_t row = blockIdx.x;
-        const int len = seq_len(lens, int(row / (int64_t(D.Hkv) * cols)), max_len);
-        combine_row<T>(part + row * splits * rec, D.d, (len + per - 1) / per, O + row * D.d, lse ? lse + row : nullptr, sh.c);
+        const int row = blockIdx.x, unit = row / cols;
+        unit_slices(D, S, seqs, unit, seq_len(lens, unit / D.Hkv, max_len), base, n);
+        combine_row<T>(part + base * step + row % cols * rec, step, D.d, n, O + int64_t(row) * D.d, lse ? lse + row : nullptr, sh.c);
         return;
     }
     const int at = int(blockIdx.x) - rows, unit = at / chunks, r0 = at % chunks * ACC_ROWS;
     const int len = seq_len(lens, unit / D.Hkv, max_len);
     if (r0 >= len) return;
-    acc_rows(A, unit, part + int64_t(unit) * cols * splits * rec, int64_t(splits) * rec, rec, (len + per - 1) / per, r0, len, sh.lse);
+    unit_slices(D, S, seqs, unit, len, base, n);
+    acc_rows(A, unit, part + base * step, rec, step, n, r0, len, sh.lse);
 }
 
 // ------------------------------------------------------------------------------------ launches
@@ -360,52 +484,72 @@ hipError_t launch_read_quant(const Dims& D, const QuantDims& Q, const int32_t* l
     return D.dtype == 1 ? run_read<bf16_t>(D, Q, lens, rows, first, K, V, st) : run_read<float>(D, Q, lens, rows, first, K, V, st);
 }
 
-// Slices: as many as fill the chip twice over when every sequence has max_len rows, of 128 rows at least (a tile per wave).
-static int quant_splits(const Dims& D, int max_len) {
-    const int units = D.B * D.Hkv, most = (max_len + 127) / 128;
-    int s = units <= 128 ? 512 / units : 2048 / units;
-    s = s < most ? s : most;
-    return s < 1 ? 1 : s > DEC_MAX_SPLITS ? DEC_MAX_SPLITS : s;
-}
 namespace {
-struct QuantPlan { int splits, per; int64_t stride; size_t part, bytes; };
+struct QuantPlan { QuantSlices s; int grid, pitch; int64_t rows; size_t part, logits, bytes; };
 }
+// Workspace: a QuantSeq per sequence, the records of `grid` workgroups, the logits.  All of them grow with max_len.
 static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
     QuantPlan P = {};
-    const int splits = quant_splits(D, max_len);
-    P.per = ((max_len + splits - 1) / splits + QT - 1) / QT * QT;
-    P.splits = (max_len + P.per - 1) / P.per;
-    P.stride = (int64_t(max_len) + QT - 1) / QT * QT;
-    const size_t rows = size_t(D.B) * D.Hq * tokens;
-    P.part = align256(rows * splits * (D.d + 2) * 4);       // grows with max_len, which P.splits does not always: a workspace for a longer one is enough
-    P.bytes = P.part + (acc ? align256(rows * size_t(P.stride) * 4) : 0);
+    const int64_t units = int64_t(D.B) * D.Hkv;
+    // two workgroups share a CU (registers), so 512 run at once; with so many units that some of these would have two slices and some one,
+    // several rounds
+    const int64_t most = units <= 256 ? 512 : units + 2048;
+    const int64_t tiles = (int64_t(max_len) + QT - 1) / QT, fine = units * ((tiles + DEC_WAVES - 1) / DEC_WAVES);
+    const float up = 1.0f + 0x1p-20f;
+    P.s.most = int(most);
+    P.s.share = float(D.Hkv) / float(most) * up;
+    P.s.safe = float(D.Hkv) / float(most - units) * up;
+    P.s.least = int((tiles + DEC_MAX_SPLITS - 1) / DEC_MAX_SPLITS);
+    if (P.s.least < DEC_WAVES) P.s.least = DEC_WAVES;          // a tile per wave
+    P.grid = int(most < fine ? most : fine);
+    if (fine <= most && P.s.least == DEC_WAVES) P.s.splits = int(fine / units);
+    P.rows = tiles * QT;
+    const size_t cols = size_t(D.G) * tokens;
+    P.part = align256(size_t(D.B) * sizeof(QuantSeq));
+    P.logits = P.part + align256(size_t(P.grid) * cols * (D.d + 2) * 4);
+    P.pitch = (D.G * tokens + 3) & ~3;
+    P.bytes = P.logits + (acc ? align256(size_t(units) * P.pitch * size_t(P.rows) * 4) : 0);
     return P;
 }
 size_t decode_quant_ws_bytes(const Dims& D, int tokens, int max_len, bool acc) { return quant_plan(D, tokens, max_len, acc).bytes; }
+// rows and tiles are counted in 32 bits
 bool decode_quant_grid_fits(const Dims& D, int tokens, int max_len) {
-    return grid_fits(int64_t(D.B) * D.Hq * tokens + int64_t(D.B) * D.Hkv * ((int64_t(max_len) + ACC_ROWS - 1) / ACC_ROWS), DEC_THREADS);
+    return max_len <= 1 << 30 && int64_t(D.B) * ((max_len + QT - 1) / QT) < int64_t(1) << 31 && grid_fits(int64_t(D.B) * D.Hq * tokens + int64_t(D.B) * D.Hkv * ((int64_t(max_len) + ACC_ROWS - 1) / ACC_ROWS), DEC_THREADS);
 }
 
 template <typename T>
 static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void* q, int tokens, const int32_t* lens, int max_len, void* O, float* lse,
                                    const float* acc_in, float* acc_out, float decay, void* ws, hipStream_t st) {
     const QuantPlan P = quant_plan(D, tokens, max_len, acc_out != nullptr);
-    float* part = reinterpret_cast<float*>(ws);
-    float* logits = acc_out ? reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + P.part) : nullptr;
+    char* w = reinterpret_cast<char*>(ws);
+    QuantSeq* seqs = reinterpret_cast<QuantSeq*>(w);
+    float* part = reinterpret_cast<float*>(w + P.part);
+    float* logits = acc_out ? reinterpret_cast<float*>(w + P.logits) : nullptr;
     const int rows = D.B * D.Hq * tokens, chunks = acc_out ? (max_len - 1) / ACC_ROWS + 1 : 0;
     AccArgs A = {};
     A.logits = logits;
     A.mul = 1.0f;
-    A.stride = P.stride;
+    A.rows = P.rows;
     A.cols = D.G * tokens;
+    A.pitch = P.pitch;
     A.in = acc_in;
     A.out = acc_out;
     A.cap = D.n;
     A.decay = decay;
-    LRSA_TIMED_LAUNCH("k_decode_quant", st, LRSA_QUANT_PICK(k_decode_quant, T), dim3(P.splits, D.B * D.Hkv), dim3(DEC_THREADS), 0, st, D, Q,
-                      (const T*)q, tokens, lens, max_len, P.per, P.splits, part, logits, P.stride);
+#define LRSA_DECODE_QUANT(DH_, FMT_, SOLE_)                                                                                              \
+    LRSA_TIMED_LAUNCH("k_decode_quant", st, (acc_out ? k_decode_quant<T, DH_, FMT_, SOLE_, true> : k_decode_quant<T, DH_, FMT_, SOLE_, false>), dim3(P.grid), dim3(DEC_THREADS), 0, st, D, Q,          \
+                      (const T*)q, tokens, lens, max_len, P.s, seqs, part, logits, P.rows, P.pitch)
+#define LRSA_DECODE_QUANT_FMT(DH_, FMT_) \
+    if (A.cols <= 16) LRSA_DECODE_QUANT(DH_, FMT_, true); else LRSA_DECODE_QUANT(DH_, FMT_, false)
+    if (Q.fmt == QUANT_INT8) {
+        if (D.d == 64) { LRSA_DECODE_QUANT_FMT(64, QUANT_INT8); } else { LRSA_DECODE_QUANT_FMT(128, QUANT_INT8); }
+    } else {
+        if (D.d == 64) { LRSA_DECODE_QUANT_FMT(64, QUANT_E4M3); } else { LRSA_DECODE_QUANT_FMT(128, QUANT_E4M3); }
+    }
+#undef LRSA_DECODE_QUANT_FMT
+#undef LRSA_DECODE_QUANT
     LRSA_TIMED_LAUNCH("k_quant_combine", st, k_quant_combine<T>, dim3(unsigned(rows + D.B * D.Hkv * chunks)), dim3(DEC_THREADS), 0, st, D, part, tokens,
-                      lens, max_len, P.per, P.splits, (T*)O, lse, A, rows, chunks);
+                      lens, max_len, P.s, seqs, (T*)O, lse, A, rows, chunks);
     return hipGetLastError();
 }
 hipError_t launch_decode_quant(const Dims& D, const QuantDims& Q, const void* q, int tokens, const int32_t* lens, int max_len, void* O, float* lse,

@@ -348,9 +348,9 @@ template <int DH> struct DecState {
     float m, l;          // of head c; l over the lane's own rows
     f32x4 o[DH / 16];
 };
-// LOGITS: `logits` is where the lane's 8 logits of the tile go, or NULL
+// LOGITS: the logits go to `out`
 template <int DH, bool LOGITS>
-__device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t, const bf16x8 (&qf)[DH / 32], int r, int r1, float c2, float* logits) {
+__device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t, const bf16x8 (&qf)[DH / 32], int r, int r1, float c2, LogitBuffer& out) {
     f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
     for (int kk = 0; kk < DH / 32; ++kk)
@@ -362,11 +362,9 @@ __device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t,
         p[j] = r + j < r1 ? s[j >> 2][j & 3] * c2 : -INFINITY;
         mx = fmaxf(mx, p[j]);
     }
-    if constexpr (LOGITS) {
-        if (logits) {      // before the factor c2: the arithmetic on p stays as it is without the stores
-            reinterpret_cast<f32x4*>(logits)[0] = s[0];
-            reinterpret_cast<f32x4*>(logits)[1] = s[1];
-        }
+    if constexpr (LOGITS) {      // before the factor c2: the arithmetic on p stays as it is without the stores
+        const float raw[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
+        keep_logits(out, raw, [](int j) { return 8 * int(threadIdx.x >> 4 & 3) + j; });
     }
     lanes_u32x2 x = pair32(__float_as_uint(mx));
     mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
@@ -410,9 +408,11 @@ __device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t,
 template <int DH, bool LOGITS>
 __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf16_t* __restrict__ q, const bf16_t* __restrict__ Kc,
                                                                 const bf16_t* __restrict__ Vc, int len, int per, int splits,
-                                                                float* __restrict__ part, float* __restrict__ logits, int64_t lstride) {
+                                                                float* __restrict__ part, float* __restrict__ logits, int64_t lrows, int pitch) {
     constexpr int CPL = DH / 16, LROW = DH + 4;              // channels per lane; the padding spreads the heads over the banks
-    __shared__ __attribute__((aligned(16))) float sO[DEC_WAVES][16][LROW];
+    constexpr int WAVE_FLOATS = LOGITS ? LOGIT_FLOATS : 16 * LROW;      // a wave's logits, then its output
+    static_assert(WAVE_FLOATS >= 16 * LROW, "LDS of a wave");
+    __shared__ __attribute__((aligned(16))) float sBuf[DEC_WAVES][WAVE_FLOATS];
     __shared__ float sM[DEC_WAVES][16], sL[DEC_WAVES][16];
     const int split = blockIdx.x, bh = blockIdx.y, b = bh / D.Hkv, h = bh % D.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, q4 = lane >> 4;
@@ -433,26 +433,27 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
         st.l = 0.0f;
 #pragma unroll
         for (int e = 0; e < CPL; ++e) st.o[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        // the next tile's loads are in flight while a tile is used
+        // The next tile's loads are in flight while a tile is used.  They are issued in every turn (the last one asks for its own tile
+        // again, from the caches): loads in a branch make the compiler wait for all of them at its end, the next tile's too
         constexpr int STEP = DEC_WAVES * DEC_TILE;
         int r = r0 + wave * DEC_TILE;
-        // tiles begin at multiples of 32 rows, and so does the end of the rows that lstride has room for
-        float* lrow = nullptr;
-        if constexpr (LOGITS) {
-            if (c < gn) lrow = logits + (int64_t(b) * D.Hq + h * D.G + g0 + c) * lstride + vr;
-        }
-        auto at = [&](int row) { return LOGITS && lrow ? lrow + row : nullptr; };
+        LogitBuffer out = {};      // tiles begin at multiples of 32 rows, and so does the end of the rows that there is room for
+        if constexpr (LOGITS) out = logit_buffer(sBuf[wave], logits + (int64_t(bh) * lrows + r) * pitch + g0, pitch, gn, STEP);
         if (r < r1) {
             DecTile<DH> A, B;
+            const int end = r + (r1 - 1 - r) / STEP * STEP;      // the wave's last tile
             load_tile<DH>(A, Kl, Vl, D.ks[2], r + kr, r + vr, r1 - 1);
             for (;;) {
-                if (r + STEP < r1) load_tile<DH>(B, Kl, Vl, D.ks[2], r + STEP + kr, r + STEP + vr, r1 - 1);
-                use_tile<DH, LOGITS>(st, A, qf, r + vr, r1, c2, at(r));
+                int next = min(r + STEP, end);
+                load_tile<DH>(B, Kl, Vl, D.ks[2], next + kr, next + vr, r1 - 1);
+                use_tile<DH, LOGITS>(st, A, qf, r + vr, r1, c2, out);
                 if ((r += STEP) >= r1) break;
-                if (r + STEP < r1) load_tile<DH>(A, Kl, Vl, D.ks[2], r + STEP + kr, r + STEP + vr, r1 - 1);
-                use_tile<DH, LOGITS>(st, B, qf, r + vr, r1, c2, at(r));
+                next = min(r + STEP, end);
+                load_tile<DH>(A, Kl, Vl, D.ks[2], next + kr, next + vr, r1 - 1);
+                use_tile<DH, LOGITS>(st, B, qf, r + vr, r1, c2, out);
                 if ((r += STEP) >= r1) break;
             }
+            if constexpr (LOGITS) flush_logits(out);
         }
         lanes_u32x2 x = pair32(__float_as_uint(st.l));
         st.l = __uint_as_float(x.x) + __uint_as_float(x.y);
@@ -464,17 +465,17 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < CPL; e += 4)
-                    *reinterpret_cast<f32x4*>(&sO[wave][c][(4 * q4 + i) * CPL + e]) = f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]};
+                    *reinterpret_cast<f32x4*>(&sBuf[wave][c * LROW + (4 * q4 + i) * CPL + e]) = f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]};
         }
         __syncthreads();
         for (int e = tid; e < gn * DH; e += DEC_THREADS) {
             const int g = e / DH, ch = e % DH;
-            float mm = sM[0][g], ll = sL[0][g], oo = sO[0][g][ch];
+            float mm = sM[0][g], ll = sL[0][g], oo = sBuf[0][g * LROW + ch];
 #pragma unroll
             for (int w = 1; w < DEC_WAVES; ++w) {
                 float a, b2;
                 merge_state(mm, ll, sM[w][g], sL[w][g], a, b2);
-                oo = oo * a + sO[w][g][ch] * b2;
+                oo = oo * a + sBuf[w][g * LROW + ch] * b2;
             }
             float* dst = part + ((int64_t(b) * D.Hq + h * D.G + g0 + g) * splits + split) * (DH + 2);
             dst[2 + ch] = oo;
@@ -489,7 +490,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
 template <typename T, bool LOGITS>
 __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __restrict__ q, const T* __restrict__ Kc,
                                                              const T* __restrict__ Vc, int len, int splits,
-                                                             float* __restrict__ part, float* __restrict__ logits, int64_t lstride) {
+                                                             float* __restrict__ part, float* __restrict__ logits, int64_t lrows, int pitch) {
     constexpr int VEC = Elem<T>::VEC;
     const int lpr = D.d / VEC, rpw = 64 / lpr;
     const int split = blockIdx.x, bh = blockIdx.y, b = bh / D.Hkv, h = bh % D.Hkv;
@@ -523,6 +524,7 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __
                 Elem<T>::load(Kh + int64_t(r) * D.ks[2] + sub * VEC, kv[u]);
                 Elem<T>::load(Vh + int64_t(r) * D.ks[2] + sub * VEC, vv[u]);
             }
+            float raw[DEC_U] = {};      // logits of the head that is the lane's number in its row
 #pragma unroll
             for (int g = 0; g < DEC_GMAX; ++g) {
                 if (g >= gn) continue;
@@ -537,13 +539,9 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __
                 for (int off = lpr >> 1; off > 0; off >>= 1)
 #pragma unroll
                     for (int u = 0; u < DEC_U; ++u) sc[u] += __shfl_xor(sc[u], off, 64);
-                if constexpr (LOGITS) {
-                    if (sub == 0) {      // before the factor c2: the arithmetic below stays as it is without the stores
-                        float* dst = logits + (int64_t(b) * D.Hq + h * D.G + g0 + g) * lstride + rb;
+                if constexpr (LOGITS) {      // before the factor c2: the arithmetic below stays as it is without the stores
 #pragma unroll
-                        for (int u = 0; u < DEC_U; ++u)
-                            if (rb + u * step < r1) dst[u * step] = sc[u];
-                    }
+                    for (int u = 0; u < DEC_U; ++u) raw[u] = sub == g ? sc[u] : raw[u];
                 }
 #pragma unroll
                 for (int u = 0; u < DEC_U; ++u) {
@@ -563,6 +561,12 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_attn(Dims D, const T* __
                 }
                 l[g] = l[g] * a + ls;
                 m[g] = mn;
+            }
+            if constexpr (LOGITS) {
+                float* dst = logits + (int64_t(bh) * lrows + rb) * pitch + g0 + sub;
+#pragma unroll
+                for (int u = 0; u < DEC_U; ++u)
+                    if (sub < gn && rb + u * step < r1) dst[u * step * pitch] = raw[u];
             }
         }
         // merge the row slots of a wave, then the waves
@@ -605,7 +609,7 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_combine(Dims D, const fl
                                                                 T* __restrict__ O, float* __restrict__ lse) {
     __shared__ CombineLds sh;
     const int64_t bhq = blockIdx.x;
-    combine_row<T>(part + bhq * splits * (D.d + 2), D.d, splits, O + bhq * D.d, lse ? lse + bhq : nullptr, sh);
+    combine_row<T>(part + bhq * splits * (D.d + 2), D.d + 2, D.d, splits, O + bhq * D.d, lse ? lse + bhq : nullptr, sh);
 }
 
 // The first B * Hq workgroups as above, the others: ACC_ROWS cache rows of a unit each.  One launch, because the two need
@@ -617,7 +621,7 @@ __global__ __launch_bounds__(DEC_THREADS) void k_decode_combine_acc(Dims D, cons
     const int rec = D.d + 2, rows = D.B * D.Hq;
     if (int(blockIdx.x) < rows) {
         const int64_t bhq = blockIdx.x;
-        combine_row<T>(part + bhq * splits * rec, D.d, splits, O + bhq * D.d, lse ? lse + bhq : nullptr, sh.c);
+        combine_row<T>(part + bhq * splits * rec, rec, D.d, splits, O + bhq * D.d, lse ? lse + bhq : nullptr, sh.c);
         return;
     }
     const int at = int(blockIdx.x) - rows, unit = at / chunks;
@@ -674,15 +678,15 @@ hipError_t launch_decode_attn_static(const Dims& D, const void* q, const void* K
 // the slices' records, and with LOGITS the logits
 template <bool LOGITS>
 static void decode_slices(const Dims& D, const void* q, const void* Kc, const void* Vc, int len, int splits, float* part, float* logits,
-                          int64_t lstride, hipStream_t st) {
+                          int64_t lrows, int pitch, hipStream_t st) {
     if (D.dtype == 1) {
         const int per = ((len + splits - 1) / splits + DEC_TILE - 1) / DEC_TILE * DEC_TILE;
         LRSA_TIMED_LAUNCH("k_decode_mfma", st, (D.d == 64 ? k_decode_mfma<64, LOGITS> : k_decode_mfma<128, LOGITS>), dim3(splits, D.B * D.Hkv),
                           dim3(DEC_THREADS), 0, st, D, (const bf16_t*)q, (const bf16_t*)Kc, (const bf16_t*)Vc, len, per, splits, part, logits,
-                          lstride);
+                          lrows, pitch);
     } else {
         LRSA_TIMED_LAUNCH("k_decode_attn", st, (k_decode_attn<float, LOGITS>), dim3(splits, D.B * D.Hkv), dim3(DEC_THREADS), 0, st, D,
-                          (const float*)q, (const float*)Kc, (const float*)Vc, len, splits, part, logits, lstride);
+                          (const float*)q, (const float*)Kc, (const float*)Vc, len, splits, part, logits, lrows, pitch);
     }
 }
 
@@ -690,7 +694,7 @@ hipError_t launch_decode_attn(const Dims& D, const void* q, const void* Kc, cons
                               float* lse, void* ws, hipStream_t st) {
     const int splits = decode_splits(D, len);
     float* part = reinterpret_cast<float*>(ws);
-    decode_slices<false>(D, q, Kc, Vc, len, splits, part, nullptr, 0, st);
+    decode_slices<false>(D, q, Kc, Vc, len, splits, part, nullptr, 0, 0, st);
     if (D.dtype == 1)
         LRSA_TIMED_LAUNCH("k_decode_combine", st, k_decode_combine<bf16_t>, dim3(D.B * D.Hq), dim3(DEC_THREADS), 0, st, D, part, splits,
                           (bf16_t*)O, lse);
@@ -703,14 +707,15 @@ hipError_t launch_decode_attn(const Dims& D, const void* q, const void* Kc, cons
 // ------------------------------------------------------------------------------------ with accumulated weights
 // A row's weights are known once every slice has been seen, so they need the logits a second time: stored in fp32, 8 bytes per
 // row and query head there and back, against 4 * d bytes of its key and value (a second read of K would be half of those).
-static int64_t logit_stride(int len) { return (int64_t(len) + DEC_TILE - 1) / DEC_TILE * DEC_TILE; }
+static int64_t logit_rows(int len) { return (int64_t(len) + DEC_TILE - 1) / DEC_TILE * DEC_TILE; }
+static int logit_pitch(const Dims& D) { return (D.G + 3) & ~3; }
 // the records' part, of the most slices that a cache of at most `len` rows is cut into: a workspace for a longer one is enough
 static size_t acc_part_bytes(const Dims& D, int len) {
     const int a = decode_fine_splits(D, len), b = decode_static_splits(D, len);
     return align256(part_bytes(D, a > b ? a : b));
 }
 size_t decode_acc_ws_bytes(const Dims& D, int len) {
-    return acc_part_bytes(D, len) + align256(size_t(D.B) * D.Hq * size_t(logit_stride(len)) * 4);
+    return acc_part_bytes(D, len) + align256(size_t(D.B) * D.Hkv * logit_pitch(D) * size_t(logit_rows(len)) * 4);
 }
 bool decode_acc_grid_fits(const Dims& D, int len) {
     return grid_fits(int64_t(D.B) * D.Hq + int64_t(D.B) * D.Hkv * ((int64_t(len) + ACC_ROWS - 1) / ACC_ROWS), DEC_THREADS);
@@ -723,13 +728,14 @@ hipError_t launch_decode_attn_acc(const Dims& D, const void* q, const void* Kc, 
     float* logits = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + acc_part_bytes(D, len));
     A.logits = logits;
     A.mul = D.scale * 1.4426950408889634f;
-    A.stride = logit_stride(len);
+    A.rows = logit_rows(len);
     A.cols = D.G;
+    A.pitch = logit_pitch(D);
     A.in = acc_in;
     A.out = acc_out;
     A.cap = D.n;
     A.decay = decay;
-    decode_slices<true>(D, q, Kc, Vc, len, splits, part, logits, A.stride, st);
+    decode_slices<true>(D, q, Kc, Vc, len, splits, part, logits, A.rows, A.pitch, st);
     const dim3 grid(unsigned(D.B * D.Hq + D.B * D.Hkv * chunks));
     if (D.dtype == 1)
         LRSA_TIMED_LAUNCH("k_decode_combine_acc", st, k_decode_combine_acc<bf16_t>, grid, dim3(DEC_THREADS), 0, st, D, part, splits, (bf16_t*)O,

@@ -1,7 +1,8 @@
 // Attention of single queries over a cache in slices of rows: the records that a slice leaves behind, how slices are
 // joined, and how the weights are added to the rows' accumulated weights.
 //
-// Record of (query row, slice): max and sum of the weights in log2 units, then d unnormalised output values, fp32.
+// Record of (query row, slice): max and sum of the weights in log2 units, then d unnormalised output values, fp32.  The slices of a
+// query row are `step` floats apart.
 #pragma once
 #include "common.h"
 
@@ -13,13 +14,14 @@ constexpr int DEC_MAX_SPLITS = 256;
 constexpr int COMB_U = 4;
 constexpr int ACC_ROWS = 4 * DEC_THREADS;     // cache rows per workgroup of the weight sums
 
-// What the weight sums read besides the records: logits [unit][cols][stride], in log2 units after the factor `mul`, -inf where
-// masked; a unit is one (sequence, KV head), its columns the query rows that read it.
+// What the weight sums read besides the records: logits [unit][rows][pitch], in log2 units after the factor `mul`, -inf where
+// masked; a unit is one (sequence, KV head), its `cols` columns the query rows that read it, in the first cols of pitch values.
+// Row by row, so that a tile's logits are one piece of memory.
 struct AccArgs {
     const float* logits;
     float mul;
-    int64_t stride;          // floats between columns, a multiple of 4
-    int cols;
+    int64_t rows;
+    int cols, pitch;         // pitch: the columns rounded up to a multiple of 4
     const float* in;         // [units][cap] or NULL: zeros
     float* out;              // [units][cap]
     int64_t cap;
@@ -27,6 +29,42 @@ struct AccArgs {
 };
 
 #if defined(__HIPCC__)
+// A wave's logits on their way to memory.  They stay in LDS until it is full or the walk over the slice ends: a stream of reads that
+// a few writes are mixed into runs at the rate of a copy, not of a read (8 requests of 32K rows of 8 bits, 4
+// columns: 119.7 us with a store per tile, 107.1, and 91.7 without logits).  Tiles of 32 rows
+// x up to 16 columns (lane l: column l % 16, 8 of the rows), `step` rows apart.
+constexpr int LOGIT_FLOATS = 4096;       // per wave: 32 tiles of 4 columns
+struct LogitBuffer {
+    float *lds, *dst;        // dst: the columns' first in the first row of the first tile that is held
+    int pitch, gn, used, most;
+    int64_t skip;            // floats between tiles in memory
+};
+__device__ __forceinline__ LogitBuffer logit_buffer(float* lds, float* dst, int pitch, int gn, int step) {
+    const int width = (gn + 3) & ~3;
+    return LogitBuffer{lds, dst, pitch, gn, 0, LOGIT_FLOATS / (32 * width), int64_t(step) * pitch};
+}
+__device__ __forceinline__ void flush_logits(LogitBuffer& B) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int pieces = (B.gn + 3) >> 2, lane = threadIdx.x & 63;
+    for (int t = 0; t < B.used; ++t, B.dst += B.skip)
+        for (int l = lane; l < 32 * pieces; l += 64) {
+            const int row = pieces == 3 ? l / 3 : l >> (pieces >> 1), part = l - row * pieces;      // what lies in pad columns is never read
+            *reinterpret_cast<float4*>(B.dst + int64_t(row) * B.pitch + part * 4) = *reinterpret_cast<const float4*>(B.lds + (t * 32 * pieces + l) * 4);
+        }
+    B.used = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+// the next tile; row(j): of the lane's value j
+template <class Row>
+__device__ __forceinline__ void keep_logits(LogitBuffer& B, const float (&p)[8], Row row) {
+    const int width = (B.gn + 3) & ~3, c = threadIdx.x & 15;
+    if (B.used == B.most) flush_logits(B);
+    if (c < width)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) B.lds[(B.used * 32 + row(j)) * width + c] = p[j];
+    ++B.used;
+}
+
 // (m, l, o) of two disjoint key sets -> of their union
 __device__ __forceinline__ void merge_state(float& m, float& l, float m2, float l2, float& a, float& b2) {
     const float mn = fmaxf(m, m2);
@@ -37,7 +75,7 @@ __device__ __forceinline__ void merge_state(float& m, float& l, float m2, float 
 }
 
 // Max, sum and the slices' weights of one query row, by a whole wave: lane l holds slices l, l + 64, ...
-__device__ __forceinline__ void merge_records(const float* src, int rec, int splits, float (&w)[DEC_MAX_SPLITS / 64], float& M, float& L) {
+__device__ __forceinline__ void merge_records(const float* src, int64_t step, int splits, float (&w)[DEC_MAX_SPLITS / 64], float& M, float& L) {
     const int lane = threadIdx.x & 63;
     float m[DEC_MAX_SPLITS / 64], l[DEC_MAX_SPLITS / 64];
     M = -INFINITY;
@@ -47,7 +85,7 @@ __device__ __forceinline__ void merge_records(const float* src, int rec, int spl
         const int s = lane + 64 * i;
         m[i] = -INFINITY; l[i] = 0.0f;
         if (s < splits) {
-            const float2 ml = *reinterpret_cast<const float2*>(src + int64_t(s) * rec);
+            const float2 ml = *reinterpret_cast<const float2*>(src + s * step);
             m[i] = ml.x; l[i] = ml.y;
         }
         M = fmaxf(M, m[i]);
@@ -69,10 +107,10 @@ struct CombineLds {
 // summed by all lanes, two channels each, COMB_U loads in flight; fixed order.  A row that sees nothing (no slices, or no
 // weight in any) gets zeros and -inf.
 template <typename T>
-__device__ __forceinline__ void combine_row(const float* src, int d, int splits, T* O, float* lse, CombineLds& sh) {
-    const int tid = threadIdx.x, lane = tid & 63, rec = d + 2;
+__device__ __forceinline__ void combine_row(const float* src, int64_t step, int d, int splits, T* O, float* lse, CombineLds& sh) {
+    const int tid = threadIdx.x, lane = tid & 63;
     float w[DEC_MAX_SPLITS / 64], M, L;
-    merge_records(src, rec, splits, w, M, L);
+    merge_records(src, step, splits, w, M, L);
 #pragma unroll
     for (int i = 0; i < DEC_MAX_SPLITS / 64; ++i)
         if (tid < 64) sh.w[lane + 64 * i] = w[i];
@@ -86,7 +124,7 @@ __device__ __forceinline__ void combine_row(const float* src, int d, int splits,
         for (int u = 0; u < COMB_U; ++u) {
             const int s = s0 + u * ways, sc = min(s, splits - 1);
             w[u] = s < splits ? sh.w[sc] : 0.0f;
-            v[u] = *reinterpret_cast<const float2*>(src + int64_t(sc) * rec + 2 + 2 * ch);
+            v[u] = *reinterpret_cast<const float2*>(src + sc * step + 2 + 2 * ch);
         }
 #pragma unroll
         for (int u = 0; u < COMB_U; ++u) {
@@ -107,39 +145,46 @@ __device__ __forceinline__ void combine_row(const float* src, int d, int splits,
 }
 
 // acc_out[r] = decay acc_in[r] + sum over the columns of exp2(logit - log2 of the column's whole weight), for rows [r0, r0 +
-// ACC_ROWS) below `len`, by one workgroup; 4 neighbouring rows per thread.  `first`: record of the unit's first column,
-// `splits` of them per column, columns `col_floats` apart.
+// ACC_ROWS) below `len`, by one workgroup; a row per thread, ACC_U rows at once.  `first`: record of the unit's first column,
+// columns `col_floats` apart.
 constexpr int ACC_COLS = 256;      // columns whose log-sum-exp is in LDS at once
-__device__ __forceinline__ void acc_rows(const AccArgs& A, int unit, const float* first, int64_t col_floats, int rec, int splits, int r0, int len,
-                                         float (&sLse)[ACC_COLS]) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = r0 + 4 * tid;
-    float4 t = {0.0f, 0.0f, 0.0f, 0.0f};
+constexpr int ACC_U = ACC_ROWS / DEC_THREADS;
+__device__ __forceinline__ void acc_rows(const AccArgs& A, int unit, const float* first, int64_t col_floats, int64_t step, int splits, int r0, int len,
+                                         float* sLse) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float* s = A.logits + int64_t(unit) * A.rows * A.pitch;
+    float sum[ACC_U] = {};
     for (int c0 = 0; c0 < A.cols; c0 += ACC_COLS) {
         const int cn = min(ACC_COLS, A.cols - c0);
         if (c0) __syncthreads();
         for (int c = wave; c < cn; c += DEC_WAVES) {
             float w[DEC_MAX_SPLITS / 64], M, L;
-            merge_records(first + (c0 + c) * col_floats, rec, splits, w, M, L);
+            merge_records(first + (c0 + c) * col_floats, step, splits, w, M, L);
             if (lane == 0) sLse[c] = L == 0.0f ? INFINITY : M + __builtin_log2f(L);
         }
         __syncthreads();
-        if (r < len) {
-            const float* s = A.logits + (int64_t(unit) * A.cols + c0) * A.stride + r;
-            for (int c = 0; c < cn; ++c) {
-                const float4 x = *reinterpret_cast<const float4*>(s + c * A.stride);
-                const float n = sLse[c];
-                t.x += __builtin_amdgcn_exp2f(__builtin_fmaf(x.x, A.mul, -n));
-                t.y += __builtin_amdgcn_exp2f(__builtin_fmaf(x.y, A.mul, -n));
-                t.z += __builtin_amdgcn_exp2f(__builtin_fmaf(x.z, A.mul, -n));
-                t.w += __builtin_amdgcn_exp2f(__builtin_fmaf(x.w, A.mul, -n));
+        for (int c = 0; c < cn; c += 4) {
+            float4 x[ACC_U];
+#pragma unroll
+            for (int u = 0; u < ACC_U; ++u)
+                x[u] = *reinterpret_cast<const float4*>(s + int64_t(min(r0 + u * DEC_THREADS + tid, len - 1)) * A.pitch + c0 + c);
+            const float4 n = *reinterpret_cast<const float4*>(&sLse[c]);
+            // a pad column's value is whatever was there
+#pragma unroll
+            for (int u = 0; u < ACC_U; ++u) {
+                sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].x, A.mul, -n.x));
+                if (c + 1 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].y, A.mul, -n.y));
+                if (c + 2 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].z, A.mul, -n.z));
+                if (c + 3 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].w, A.mul, -n.w));
             }
         }
     }
-    const float v[4] = {t.x, t.y, t.z, t.w};
-    const int64_t at = int64_t(unit) * A.cap + r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (r + i < len) A.out[at + i] = A.in ? __builtin_fmaf(A.decay, A.in[at + i], v[i]) : v[i];
+    for (int u = 0; u < ACC_U; ++u) {
+        const int r = r0 + u * DEC_THREADS + tid;
+        const int64_t at = int64_t(unit) * A.cap + r;
+        if (r < len) A.out[at] = A.in ? __builtin_fmaf(A.decay, A.in[at], sum[u]) : sum[u];
+    }
 }
 #endif
 
