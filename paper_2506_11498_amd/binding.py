@@ -354,31 +354,32 @@ def _stream_of(index: int):
     return _stream() if _raw_stream is None else _raw_stream(index)
 
 
-def _flat(name: str, t: Optional[torch.Tensor], shape, dtype, device) -> Optional[int]:
+def _flat(name: str, t: Optional[torch.Tensor], shape, dtype, index: int) -> Optional[int]:
     """The address of a contiguous tensor of that shape."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        _expect(name, t, shape, None, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        _expect(name, t, shape, None, dtype, torch.device("cuda", index))
     return t.data_ptr()
 
 
-def _rows(name: str, t: Optional[torch.Tensor], shape, stride, dtype, device) -> Optional[int]:
+def _rows(name: str, t: Optional[torch.Tensor], shape, stride, dtype, index: int) -> Optional[int]:
     """The address of a tensor of that shape and those strides."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not dtype or t.device != device or t.stride() != stride:
-        _expect(name, t, shape, stride, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or t.stride() != stride:
+        _expect(name, t, shape, stride, dtype, torch.device("cuda", index))
     return t.data_ptr()
 
 
-def _call_ws(need, device, ws: Optional[torch.Tensor]):
-    """Address and bytes of the caller's workspace, or of one for this call (then the tensor, too)."""
-    if ws is None:
-        ws = torch.empty(need(), dtype=torch.uint8, device=device)
-    elif ws.device != device or not ws.is_contiguous():
-        raise ValueError(f"ws must be contiguous and on {device}")
-    return ws, ws.data_ptr(), ws.nbytes
+def _own_ws(need: int, index: int) -> torch.Tensor:
+    return torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
+
+
+def _ws_at(ws: torch.Tensor, index: int) -> int:
+    if ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on cuda:{index}")
+    return ws.data_ptr()
 
 
 def decode_attn_acc_ws_bytes(p: LrsaParams, length: int) -> int:
@@ -397,11 +398,12 @@ def lrsa_decode_attn_acc(p: LrsaParams, q: torch.Tensor, Kc: torch.Tensor, Vc: t
     if lse is None:
         lse = torch.empty((B, Hq), dtype=f32, device=dev)
     one, kv, st, acc = (B, Hq, d), (B, Hkv, cap, d), (*ks, 1), (B, Hkv, cap)
-    args = (_flat("q", q, one, dt, dev), _rows("Kc", Kc, kv, st, dt, dev), _rows("Vc", Vc, kv, st, dt, dev), length,
-            _flat("acc_in", acc_in, acc, f32, dev), _flat("acc_out", acc_out, acc, f32, dev), decay, _flat("O", O, one, dt, dev),
-            _flat("lse", lse, (B, Hq), f32, dev))
-    ws, at, nb = _call_ws(lambda: decode_attn_acc_ws_bytes(p, length), dev, ws)
-    _check(lib().lrsa_decode_attn_acc(ctypes.byref(p), *args, at, nb, _stream_of(index)))
+    args = (_flat("q", q, one, dt, index), _rows("Kc", Kc, kv, st, dt, index), _rows("Vc", Vc, kv, st, dt, index), length,
+            _flat("acc_in", acc_in, acc, f32, index), _flat("acc_out", acc_out, acc, f32, index), decay, _flat("O", O, one, dt, index),
+            _flat("lse", lse, (B, Hq), f32, index))
+    if ws is None:
+        ws = _own_ws(decode_attn_acc_ws_bytes(p, length), index)
+    _check(lib().lrsa_decode_attn_acc(ctypes.byref(p), *args, _ws_at(ws, index), ws.nbytes, _stream_of(index)))
     return O, lse, acc_out
 
 
@@ -418,11 +420,12 @@ def lrsa_cache_evict(p: LrsaParams, Kc: torch.Tensor, Vc: torch.Tensor, pos: Opt
     index, dev, i32, f32 = _here(Kc), Kc.device, torch.int32, torch.float32
     (B, _, Hkv, cap, d), dt, ks = _read(p)
     kv, st, lst, new = (B, Hkv, cap, d), (*ks, 1), (B, Hkv, cap), ctypes.c_int32(0)
-    args = (_rows("Kc", Kc, kv, st, dt, dev), _rows("Vc", Vc, kv, st, dt, dev), _flat("pos", pos, lst, i32, dev), _flat("acc", acc, lst, f32, dev),
-            length, budget, recent, _rows("Ko", Ko, kv, st, dt, dev), _rows("Vo", Vo, kv, st, dt, dev), _flat("pos_o", pos_o, lst, i32, dev),
-            _flat("acc_o", acc_o, lst, f32, dev))
-    ws, at, nb = _call_ws(lambda: cache_evict_ws_bytes(p, length, budget), dev, ws)
-    _check(lib().lrsa_cache_evict(ctypes.byref(p), *args, ctypes.byref(new), at, nb, _stream_of(index)))
+    args = (_rows("Kc", Kc, kv, st, dt, index), _rows("Vc", Vc, kv, st, dt, index), _flat("pos", pos, lst, i32, index), _flat("acc", acc, lst, f32, index),
+            length, budget, recent, _rows("Ko", Ko, kv, st, dt, index), _rows("Vo", Vo, kv, st, dt, index), _flat("pos_o", pos_o, lst, i32, index),
+            _flat("acc_o", acc_o, lst, f32, index))
+    if ws is None:
+        ws = _own_ws(cache_evict_ws_bytes(p, length, budget), index)
+    _check(lib().lrsa_cache_evict(ctypes.byref(p), *args, ctypes.byref(new), _ws_at(ws, index), ws.nbytes, _stream_of(index)))
     return new.value
 
 
@@ -475,9 +478,9 @@ def lrsa_cache_append_quant(p: LrsaParams, cache: QuantCache, K: torch.Tensor, V
     (B, _, Hkv, cap, d), dt, ks = _read(p)
     tokens = K.shape[2]
     kv, st = (B, Hkv, tokens, d), (*ks, 1)
-    _check(lib().lrsa_cache_append_quant(ctypes.byref(p), cache._as("cache", (B, Hkv, cap, d), dev), _rows("K", K, kv, st, dt, dev),
-                                         _rows("V", V, kv, st, dt, dev), tokens, _flat("lens", lens, (B,), i32, dev),
-                                         _flat("counts", counts, (B,), i32, dev), _stream_of(index)))
+    _check(lib().lrsa_cache_append_quant(ctypes.byref(p), cache._as("cache", (B, Hkv, cap, d), dev), _rows("K", K, kv, st, dt, index),
+                                         _rows("V", V, kv, st, dt, index), tokens, _flat("lens", lens, (B,), i32, index),
+                                         _flat("counts", counts, (B,), i32, index), _stream_of(index)))
 
 
 def lrsa_cache_read_quant(p: LrsaParams, cache: QuantCache, lens: torch.Tensor, rows: int, first: Optional[torch.Tensor] = None,
@@ -488,8 +491,8 @@ def lrsa_cache_read_quant(p: LrsaParams, cache: QuantCache, lens: torch.Tensor, 
     (B, _, Hkv, cap, d), dt, ks = _read(p)
     kv, st = (B, Hkv, rows, d), (*ks, 1)
     K, V = (torch.empty_strided(kv, st, dtype=dt, device=dev) if t is None else t for t in (K, V))
-    _check(lib().lrsa_cache_read_quant(ctypes.byref(p), cache._as("cache", (B, Hkv, cap, d), dev), _flat("lens", lens, (B,), i32, dev), rows,
-                                       _flat("first", first, (B,), i32, dev), _rows("K", K, kv, st, dt, dev), _rows("V", V, kv, st, dt, dev),
+    _check(lib().lrsa_cache_read_quant(ctypes.byref(p), cache._as("cache", (B, Hkv, cap, d), dev), _flat("lens", lens, (B,), i32, index), rows,
+                                       _flat("first", first, (B,), i32, index), _rows("K", K, kv, st, dt, index), _rows("V", V, kv, st, dt, index),
                                        _stream_of(index)))
     return K, V
 
@@ -513,11 +516,12 @@ def lrsa_decode_attn_quant(p: LrsaParams, q: torch.Tensor, cache: QuantCache, le
         O = torch.empty(shape, dtype=q.dtype, device=dev)
     if lse is None:
         lse = torch.empty(rows, dtype=f32, device=dev)
-    args = (cache._as("cache", (B, Hkv, cap, d), dev), _flat("q", q, shape, dt, dev), tokens, _flat("lens", lens, (B,), torch.int32, dev), max_len,
-            _flat("acc_in", acc_in, acc, f32, dev), _flat("acc_out", acc_out, acc, f32, dev), decay, _flat("O", O, shape, dt, dev),
-            _flat("lse", lse, rows, f32, dev))
-    ws, at, nb = _call_ws(lambda: decode_attn_quant_ws_bytes(p, tokens, max_len, acc_out is not None), dev, ws)
-    _check(lib().lrsa_decode_attn_quant(ctypes.byref(p), *args, at, nb, _stream_of(index)))
+    args = (cache._as("cache", (B, Hkv, cap, d), dev), _flat("q", q, shape, dt, index), tokens, _flat("lens", lens, (B,), torch.int32, index), max_len,
+            _flat("acc_in", acc_in, acc, f32, index), _flat("acc_out", acc_out, acc, f32, index), decay, _flat("O", O, shape, dt, index),
+            _flat("lse", lse, rows, f32, index))
+    if ws is None:
+        ws = _own_ws(decode_attn_quant_ws_bytes(p, tokens, max_len, acc_out is not None), index)
+    _check(lib().lrsa_decode_attn_quant(ctypes.byref(p), *args, _ws_at(ws, index), ws.nbytes, _stream_of(index)))
     return O, lse
 
 
@@ -528,11 +532,12 @@ def lrsa_cache_evict_quant(p: LrsaParams, cache: QuantCache, pos: Optional[torch
     index, dev, i32, f32 = _here(acc), acc.device, torch.int32, torch.float32
     (B, _, Hkv, cap, d), _, _ = _read(p)
     kv, lst = (B, Hkv, cap, d), (B, Hkv, cap)
-    args = (cache._as("cache", kv, dev), _flat("pos", pos, lst, i32, dev), _flat("acc", acc, lst, f32, dev), _flat("lens", lens, (B,), i32, dev), max_len,
-            budget, recent, out._as("out", kv, dev), _flat("pos_o", pos_o, lst, i32, dev), _flat("acc_o", acc_o, lst, f32, dev),
-            _flat("lens_o", lens_o, (B,), i32, dev))
-    ws, at, nb = _call_ws(lambda: cache_evict_ws_bytes(p, max_len, budget), dev, ws)
-    _check(lib().lrsa_cache_evict_quant(ctypes.byref(p), *args, at, nb, _stream_of(index)))
+    args = (cache._as("cache", kv, dev), _flat("pos", pos, lst, i32, index), _flat("acc", acc, lst, f32, index), _flat("lens", lens, (B,), i32, index), max_len,
+            budget, recent, out._as("out", kv, dev), _flat("pos_o", pos_o, lst, i32, index), _flat("acc_o", acc_o, lst, f32, index),
+            _flat("lens_o", lens_o, (B,), i32, index))
+    if ws is None:
+        ws = _own_ws(cache_evict_ws_bytes(p, max_len, budget), index)
+    _check(lib().lrsa_cache_evict_quant(ctypes.byref(p), *args, _ws_at(ws, index), ws.nbytes, _stream_of(index)))
 
 
 def lrsa_attn_fwd(p: LrsaParams, Q, K, V, idx, O: Optional[torch.Tensor] = None,

@@ -509,7 +509,7 @@ int check_evict(const char* who, const lrsa::Dims& D, int32_t len, int32_t budge
     if (len < 0 || len > D.n) return fail(LRSA_ERR_INVALID_ARG, "%s: length %d outside [0, cap=%d]", who, len, D.n);
     if (recent < 0 || budget < 1 || budget > D.n || (int64_t)D.S + recent > budget)
         return fail(LRSA_ERR_INVALID_ARG, "%s: budget %d must be in [1, cap=%d] and hold sink %d and recent %d", who, budget, D.n, D.S, recent);
-    if (!lrsa::cache_evict_grid_fits(D, budget)) return fail(LRSA_ERR_UNSUPPORTED, "%s: budget %d is beyond the launch grid limits", who, budget);
+    if (!lrsa::cache_evict_grid_fits(D, len, budget)) return fail(LRSA_ERR_UNSUPPORTED, "%s: length %d or budget %d is beyond the launch grid limits", who, len, budget);
     return LRSA_OK;
 }
 int check_evict_lists(const char* who, const int32_t* pos, const float* acc, const int32_t* pos_o, const float* acc_o) {

@@ -26,22 +26,31 @@ struct EvictArgs {
 };
 __device__ __forceinline__ int evict_len(const EvictArgs& E, int b) { return E.lens ? max(0, min(E.lens[b], E.len)) : E.len; }
 
-// Order of weights as of unsigned numbers, with room for 0 and the largest: those are rows that are not there and rows that
-// stay whatever their weight.  -0 equals 0.
+// Order of weights as of unsigned numbers.  -0 equals 0; what is no number goes to either end.  Of weights, the first 11 bits are
+// neither all zeros nor all ones: those are rows that are not there and rows that stay whatever their weight.
+constexpr uint32_t KEY_ABSENT = 0u, KEY_STAYS = 0xffffffffu;
 __device__ __forceinline__ uint32_t weight_key(float x) {
     uint32_t u = __float_as_uint(x + 0.0f);
     u ^= u >> 31 ? 0xffffffffu : 0x80000000u;
-    return min(max(u, 1u), 0xfffffffeu);
+    return min(max(u, 0x00400000u), 0xffbfffffu);
 }
 
-// Radix select of the budget-th largest key (digits of 11, 11 and 10 bits: a weight's first 11 bits are sign, exponent and two
-// bits of fraction, which spreads the LDS atomics), then an ordered compaction.  Integer work only: deterministic.
+// Radix select of the smallest key that stays (digits of 11, 11 and 10 bits: a weight's first 11 bits are sign, exponent and two
+// bits of fraction, which spreads the LDS atomics; two histograms, a lane's by its number, so that equal keys collide in 32
+// lanes and not in 64), then an ordered compaction by ballots.  Integer work only: deterministic.
+// A wave holds 64 * KPT neighbouring rows' keys in registers, four neighbours per lane and group, so the weights are read once; a cache of
+// more than 16 waves' keys is taken in parts, read again in every pass.  One workgroup, because its passes depend on each other; bound by
+// what one CU reads and by some 20 instructions and an LDS atomic per row: 32K rows 16 us, 4.5K rows 5.5 us (keys in LDS instead: 18; an
+// atomic behind a branch per row and pass: 22; keys read again in every pass, as a longer cache does: 43).
+template <int KPT>
 __global__ __launch_bounds__(EVICT_THREADS) void k_evict_select(Dims D, EvictArgs E, int32_t* __restrict__ keep) {
-    __shared__ int hist[EVICT_BINS];
-    __shared__ int sm[EVICT_THREADS / 64];
+    constexpr int WAVES = EVICT_THREADS / 64, PART = EVICT_THREADS * KPT, GROUPS = KPT / 4, COPIES = 2, PITCH = EVICT_BINS + 4;
+    __shared__ __attribute__((aligned(16))) int hist[COPIES * PITCH + 64];
+    __shared__ int sm[WAVES];
+    __shared__ int2 s_count[WAVES];
     __shared__ uint32_t s_prefix;
     __shared__ int s_need, s_all;
-    const int unit = blockIdx.x, b = unit / D.Hkv, tid = threadIdx.x;
+    const int unit = blockIdx.x, b = unit / D.Hkv, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int len = evict_len(E, b);
     if (E.lens_o && unit % D.Hkv == 0 && tid == 0) E.lens_o[b] = min(len, E.budget);
     keep += int64_t(unit) * E.budget;
@@ -49,64 +58,182 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_evict_select(Dims D, EvictArg
         for (int r = tid; r < len; r += EVICT_THREADS) keep[r] = r;
         return;
     }
-    const float* acc = E.acc + int64_t(unit) * E.cap;
-    const int tail = len - E.recent;
-    auto key = [&](int r) { return r < D.S || r >= tail ? 0xffffffffu : weight_key(acc[r]); };
-    uint32_t prefix = 0, mask = 0;
-    int need = E.budget;
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < EVICT_BINS; i += EVICT_THREADS) hist[i] = 0;
-        __syncthreads();
-        for (int r = tid; r < len; r += EVICT_THREADS) {
-            const uint32_t k = key(r);
-            if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1);
+    struct __attribute__((packed, aligned(4))) Four { uint32_t v[4]; };
+    const uint32_t* acc = reinterpret_cast<const uint32_t*>(E.acc + int64_t(unit) * E.cap);
+    const int tail = len - E.recent, parts = (len + PART - 1) / PART;
+    uint4 k[GROUPS];                         // of group g: rows 256 g + 4 lane .. + 3 of the wave's
+    auto first_row = [&](int part) { return part * PART + wave * 64 * KPT; };
+    auto load = [&](int part) {
+        const int first = first_row(part);
+        if (first + 64 * KPT <= len) {
+            const uint32_t* src = acc + first;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const Four f = *reinterpret_cast<const Four*>(src + 256 * g + uint32_t(4 * lane));
+                // opaque: or the compiler makes one set of loads, word by word, of this branch's and the other's
+                k[g] = uint4{as_loaded(f.v[0]), as_loaded(f.v[1]), as_loaded(f.v[2]), as_loaded(f.v[3])};
+            }
+        } else {
+            const uint32_t* src = acc + min(first, len - 1);
+            const uint32_t last = max(len - 1 - first, 0);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const uint32_t r = 256 * g + 4 * lane;
+                k[g] = uint4{src[min(r, last)], src[min(r + 1, last)], src[min(r + 2, last)], src[min(r + 3, last)]};
+            }
         }
-        __syncthreads();
-        const int top = EVICT_BINS - 1 - 2 * tid, c0 = hist[top], c1 = hist[top - 1];
-        int total;
-        const int above = block_exscan<EVICT_THREADS>(c0 + c1, sm, &total);
-        if (above < need && need <= above + c0) {
-            s_prefix = prefix | uint32_t(top) << shift;
-            s_need = need - above;
-            s_all = need - above == c0;
-        } else if (above + c0 < need && need <= above + c0 + c1) {
-            s_prefix = prefix | uint32_t(top - 1) << shift;
-            s_need = need - above - c0;
-            s_all = need - above - c0 == c1;
+        const bool plain = first >= D.S && first + 64 * KPT <= tail;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            uint32_t v[4] = {k[g].x, k[g].y, k[g].z, k[g].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = weight_key(__uint_as_float(v[i]));
+            if (!plain)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = first + 256 * g + 4 * lane + i;
+                    v[i] = r >= len ? KEY_ABSENT : r < D.S || r >= tail ? KEY_STAYS : v[i];
+                }
+            k[g] = uint4{v[0], v[1], v[2], v[3]};
         }
-        __syncthreads();
-        prefix = s_prefix;
-        need = s_need;
-        mask |= ((1u << bits) - 1) << shift;
-        if (s_all) break;
+    };
+    auto each_group = [&](auto use) {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) use(g, k[g]);
+    };
+    if (parts == 1) load(0);
+    // Rows between that stay: those above the threshold on the decided bits, and the first `need` that equal it.  None: a threshold
+    // between weights and KEY_STAYS
+    uint32_t prefix = 0xffc00000u, mask = 0xffe00000u;
+    int need = E.budget - D.S - E.recent;
+    if (need > 0) {
+        prefix = mask = 0;
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t bins = pass == 2 ? 1023u : 2047u;
+            for (int i = tid; i < COPIES * PITCH / 4; i += EVICT_THREADS) reinterpret_cast<int4*>(hist)[i] = int4{0, 0, 0, 0};
+            __syncthreads();
+            for (int part = 0; part < parts; ++part) {
+                if (parts > 1) load(part);
+                const uint32_t own = uint32_t((lane & (COPIES - 1)) * PITCH), dust = uint32_t(COPIES * PITCH + lane);
+                if (pass == 0 && first_row(part) >= D.S && first_row(part) + 64 * KPT <= tail)
+                    each_group([&](int, const uint4& k4) {       // all rows are there, and none stays whatever its weight
+                        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) atomicAdd(&hist[own + (k[i] >> 21)], 1);
+                    });
+                else if (pass == 0)
+                    each_group([&](int, const uint4& k4) {
+                        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) atomicAdd(&hist[k[i] + 1u > 1u ? own + (k[i] >> 21) : dust], 1);
+                    });
+                else
+                    each_group([&](int, const uint4& k4) {
+                        // few keys match: one atomic for the first of a lane's four (the lane's own dustbin if there is none), without a branch
+                        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+                        bool m[4], seen = false, more = false;
+                        uint32_t at = dust;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            m[i] = (k[i] & mask) == prefix;
+                            more |= seen && m[i];
+                            at = !seen && m[i] ? own + ((k[i] >> shift) & bins) : at;
+                            m[i] = m[i] && seen;
+                            seen |= (k[i] & mask) == prefix;
+                        }
+                        atomicAdd(&hist[at], 1);
+                        if (__builtin_amdgcn_ballot_w64(more) != 0)
+#pragma unroll
+                            for (int i = 1; i < 4; ++i)
+                                if (m[i]) atomicAdd(&hist[own + ((k[i] >> shift) & bins)], 1);
+                    });
+            }
+            __syncthreads();
+            const int top = EVICT_BINS - 1 - 2 * tid;
+            int c0 = 0, c1 = 0;
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const int2 c = *reinterpret_cast<const int2*>(&hist[i * PITCH + top - 1]);
+                c0 += c.y;
+                c1 += c.x;
+            }
+            int total;
+            const int above = block_exscan<EVICT_THREADS>(c0 + c1, sm, &total);
+            if (above < need && need <= above + c0) {
+                s_prefix = prefix | uint32_t(top) << shift;
+                s_need = need - above;
+                s_all = need - above == c0;
+            } else if (above + c0 < need && need <= above + c0 + c1) {
+                s_prefix = prefix | uint32_t(top - 1) << shift;
+                s_need = need - above - c0;
+                s_all = need - above - c0 == c1;
+            }
+            __syncthreads();
+            prefix = s_prefix;
+            need = s_need;
+            mask |= bins << shift;
+            if (s_all) {                     // every key that equals it is wanted: above the number below it, in what is decided
+                prefix -= mask & (0u - mask);
+                need = 0;
+                break;
+            }
+        }
     }
-    // larger than the threshold, or among the first `need` equal to it on the decided bits
-    constexpr int RUN = 4;
-    int gt_seen = 0, eq_seen = 0;
-    for (int b0 = 0; b0 < len; b0 += RUN * EVICT_THREADS) {
-        const int r0 = b0 + tid * RUN;
-        uint32_t km[RUN];
-        int ngt = 0, neq = 0;
+    int above = 0, equal = 0;                // of the rows before
+    for (int part = 0; part < parts; ++part) {
+        if (parts > 1) load(part);
+        int na = 0, ne = 0;                  // of the wave
+        each_group([&](int, const uint4& k4) {
+            const uint32_t k[4] = {k4.x & mask, k4.y & mask, k4.z & mask, k4.w & mask};
 #pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            km[i] = r0 + i < len ? key(r0 + i) & mask : 0u;
-            ngt += (r0 + i < len && km[i] > prefix) ? 1 : 0;
-            neq += (r0 + i < len && km[i] == prefix) ? 1 : 0;
-        }
-        int total;
-        const int before = block_exscan<EVICT_THREADS>(ngt | (neq << 16), sm, &total);
-        int g = gt_seen + (before & 0xffff), e = eq_seen + (before >> 16);
+            for (int i = 0; i < 4; ++i) na += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[i] > prefix));
+            if (need > 0)
 #pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            if (r0 + i >= len) break;
-            const bool is_gt = km[i] > prefix, is_eq = km[i] == prefix;
-            if (is_gt || (is_eq && e < need)) keep[g + min(e, need)] = r0 + i;
-            g += is_gt ? 1 : 0;
-            e += is_eq ? 1 : 0;
+                for (int i = 0; i < 4; ++i) ne += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[i] == prefix));
+        });
+        __syncthreads();
+        if (lane == 0) s_count[wave] = int2{na, ne};
+        __syncthreads();
+        int a = above, e = equal;
+        {
+            const int2 c = lane < WAVES ? s_count[lane] : int2{0, 0};
+            const int sa = wave_iscan(c.x), se = wave_iscan(c.y);
+            a += __builtin_amdgcn_readlane(sa, wave) - na;
+            e += __builtin_amdgcn_readlane(se, wave) - ne;
+            above += __builtin_amdgcn_readlane(sa, 63);
+            equal += __builtin_amdgcn_readlane(se, 63);
         }
-        gt_seen += total & 0xffff;
-        eq_seen += total >> 16;
+        const int r0 = first_row(part) + 4 * lane;
+        each_group([&](int g, const uint4& k4) {
+            const uint32_t k[4] = {k4.x & mask, k4.y & mask, k4.z & mask, k4.w & mask};
+            int my_a = a, my_e = e;          // rows above, rows equal before the lane's first one
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t m = __builtin_amdgcn_ballot_w64(k[i] > prefix);
+                my_a = __builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), my_a));
+                a += __builtin_popcountll(m);
+            }
+            if (need == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k[i] > prefix) keep[my_a++] = r0 + 256 * g + i;
+                return;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t m = __builtin_amdgcn_ballot_w64(k[i] == prefix);
+                my_e = __builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), my_e));
+                e += __builtin_popcountll(m);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool ia = k[i] > prefix, ie = k[i] == prefix;
+                if (ia || (ie && my_e < need)) keep[my_a + min(my_e, need)] = r0 + 256 * g + i;
+                my_a += ia ? 1 : 0;
+                my_e += ie ? 1 : 0;
+            }
+        });
     }
 }
 
@@ -121,7 +248,8 @@ __device__ __forceinline__ void evict_lists(const EvictArgs& E, int unit, int le
     }
 }
 
-// 16 bytes per thread
+// 16 bytes per thread.  Bound by memory, which reads and writes at the rate of a copy: 4 x 8 heads, 8192 rows of 512 bytes, 52.8 us = 5.1 TB/s
+// (58.3 through the caches; several rows per thread: 61).
 template <typename T>
 __global__ __launch_bounds__(256) void k_evict_rows(Dims D, EvictArgs E, const T* __restrict__ K, const T* __restrict__ V, const int32_t* __restrict__ keep,
                                                     T* __restrict__ Ko, T* __restrict__ Vo) {
@@ -133,18 +261,21 @@ __global__ __launch_bounds__(256) void k_evict_rows(Dims D, EvictArgs E, const T
         return;
     }
     const int lpr = D.d / Elem<T>::VEC;
-    const int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t i = e / lpr;
+    const int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x, i = e / lpr;
     if (i >= min(len, E.budget)) return;
     const int64_t at = b * D.ks[0] + h * D.ks[1] + e % lpr * Elem<T>::VEC;
-    *reinterpret_cast<uint4*>((z ? Vo : Ko) + at + i * D.ks[2]) = *reinterpret_cast<const uint4*>((z ? V : K) + at + int64_t(keep[i]) * D.ks[2]);
+    stream_store((z ? Vo : Ko) + at + i * D.ks[2], stream_load((z ? V : K) + at + keep[i] * D.ks[2]));
 }
 
-// One workgroup per block of the new cache
+// One workgroup: 256 neighbouring rows of the new cache, of one (sequence, KV head, K or V), which are whole blocks of it; 16 codes of a
+// row per lane.  List, rows and scales are a chain of three reads, so many rows are asked for at once: 8 x 8 heads,
+// 8192 rows, 55 us = 4.9 TB/s (a block per workgroup: 119; through the caches the rows' next reader waits for the writes: 55 us here, but 87
+// instead of 77 us there).
+constexpr int EVICT_WG_ROWS = 256;
 template <int DH, int FMT>
 __global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantDims Q, const int32_t* __restrict__ keep, QuantDims N) {
-    constexpr int LPR = DH / 8, RPP = 256 / LPR, PASSES = QUANT_MAX_BLOCK / RPP;
-    __shared__ float sm[4];
+    constexpr int LPR = DH / 16, RPP = 256 / LPR, PASSES = EVICT_WG_ROWS / RPP, WROWS = 64 / LPR;      // rows of a wave and pass: 8 or 16
+    __shared__ float s_top[EVICT_WG_ROWS / WROWS], s_scale[EVICT_WG_ROWS / 16];
     const int z = blockIdx.y, unit = blockIdx.z, b = unit / D.Hkv, h = unit % D.Hkv;
     const int len = evict_len(E, b);
     keep += int64_t(unit) * E.budget;
@@ -152,44 +283,62 @@ __global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantD
         evict_lists(E, unit, len, keep, blockIdx.x, gridDim.x);
         return;
     }
-    const int64_t row0 = int64_t(blockIdx.x) << N.log_block;
-    const int rows = int(min(int64_t(N.block), min(len, E.budget) - row0));
+    const int64_t row0 = int64_t(blockIdx.x) * EVICT_WG_ROWS;
+    const int rows = int(min(int64_t(EVICT_WG_ROWS), min(len, E.budget) - row0));
     if (rows <= 0) return;
-    const int sub = threadIdx.x % LPR, rg = threadIdx.x / LPR;
-    const uint8_t* src = (z ? Q.V : Q.K) + b * Q.st[0] + h * Q.st[1] + sub * 8;
+    const int tid = threadIdx.x, sub = tid % LPR, rg = tid / LPR;
+    const uint8_t* src = (z ? Q.V : Q.K) + b * Q.st[0] + h * Q.st[1] + sub * 16;
     const float* scales = (z ? Q.Vs : Q.Ks) + int64_t(unit) * Q.nb;
-    float v[PASSES][8], top = 0.0f;
+    int from[PASSES];
+    uint4 codes[PASSES];
+    float scale[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) from[p] = keep[row0 + min(p * RPP + rg, rows - 1)];      // rows past the end repeat the last one
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-        const int r = p * RPP + rg;
-        if (r < rows) {
-            const int from = keep[row0 + r];
-            const float s = scales[from >> Q.log_block];
-            code_values<FMT>(*reinterpret_cast<const uint2*>(src + from * Q.st[2]), v[p]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[p][i] *= s;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[p][i] = 0.0f;
-        }
+        codes[p] = stream_load(src + from[p] * Q.st[2]);
+        scale[p] = scales[from[p] >> Q.log_block];
     }
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p)
+    for (int p = 0; p < PASSES; ++p) {
+        float lo[8], hi[8], top = 0.0f;
+        code_values<FMT>(uint2{as_loaded(codes[p].x), as_loaded(codes[p].y)}, lo);
+        code_values<FMT>(uint2{as_loaded(codes[p].z), as_loaded(codes[p].w)}, hi);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[p][i]));
-    const float s = quant_scale<FMT>(block_max<256>(top, sm));
-    const float inv = 1.0f / s;
-    if (threadIdx.x == 0) (z ? N.Vs : N.Ks)[int64_t(unit) * N.nb + blockIdx.x] = s;
-    uint8_t* dst = (z ? N.V : N.K) + b * N.st[0] + h * N.st[1] + row0 * N.st[2] + sub * 8;
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(lo[i]), fabsf(hi[i])));
+        top = wave_max(p * RPP + rg < rows ? top * scale[p] : 0.0f);
+        if ((tid & 63) == 0) s_top[p * 4 + (tid >> 6)] = top;          // rows WROWS * (4 p + wave) ..
+    }
+    __syncthreads();
+    const int per = N.block / WROWS;                                   // such groups of rows in a block
+    if (tid * N.block < rows) {
+        float top = 0.0f;
+        for (int i = 0; i < per; ++i) top = fmaxf(top, s_top[tid * per + i]);
+        const float s = quant_scale<FMT>(top);
+        s_scale[tid] = s;
+        (z ? N.Vs : N.Ks)[int64_t(unit) * N.nb + (row0 >> N.log_block) + tid] = s;
+    }
+    __syncthreads();
+    uint8_t* dst = (z ? N.V : N.K) + b * N.st[0] + h * N.st[1] + row0 * N.st[2] + sub * 16;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int r = p * RPP + rg;
-        if (r < rows) *reinterpret_cast<uint2*>(dst + r * N.st[2]) = make_codes<FMT>(v[p], inv);
+        if (r >= rows) continue;
+        const float ratio = scale[p] * (1.0f / s_scale[r >> N.log_block]);      // exact for powers of two
+        uint4 c = codes[p];
+        if (ratio != 1.0f) {
+            float lo[8], hi[8];
+            code_values<FMT>(uint2{as_loaded(c.x), as_loaded(c.y)}, lo);
+            code_values<FMT>(uint2{as_loaded(c.z), as_loaded(c.w)}, hi);
+            const uint2 a = make_codes<FMT>(lo, ratio), e = make_codes<FMT>(hi, ratio);
+            c = uint4{a.x, a.y, e.x, e.y};
+        }
+        stream_store(dst + r * N.st[2], c);
     }
 }
 
 size_t cache_evict_ws_bytes(const Dims& D, int budget) { return align256(size_t(D.B) * D.Hkv * budget * 4); }
-bool cache_evict_grid_fits(const Dims& D, int budget) { return grid_fits((int64_t(budget) * 32 + 255) / 256 + 1, 256); }
+bool cache_evict_grid_fits(const Dims&, int len, int budget) { return len <= 1 << 30 && grid_fits(int64_t(budget) / 8 + 1, 256); }
 
 static EvictArgs evict_args(const Dims& D, const int32_t* lens, int len, int budget, int recent, const int32_t* pos, const float* acc, int32_t* pos_o,
                             float* acc_o, int32_t* lens_o) {
@@ -207,10 +356,16 @@ static EvictArgs evict_args(const Dims& D, const int32_t* lens, int len, int bud
     return E;
 }
 
+static void launch_select(const Dims& D, const EvictArgs& E, int32_t* keep, hipStream_t st) {
+    const int per = (E.len + EVICT_THREADS - 1) / EVICT_THREADS;      // keys per thread
+    LRSA_TIMED_LAUNCH("k_evict_select", st, (per <= 4 ? k_evict_select<4> : per <= 8 ? k_evict_select<8> : per <= 16 ? k_evict_select<16> :
+                      k_evict_select<32>), dim3(D.B * D.Hkv), dim3(EVICT_THREADS), 0, st, D, E, keep);
+}
+
 template <typename T>
 static hipError_t run_evict(const Dims& D, const EvictArgs& E, const void* K, const void* V, void* Ko, void* Vo, int32_t* keep, hipStream_t st) {
     const int rows = E.len < E.budget ? E.len : E.budget;
-    LRSA_TIMED_LAUNCH("k_evict_select", st, k_evict_select, dim3(D.B * D.Hkv), dim3(EVICT_THREADS), 0, st, D, E, keep);
+    launch_select(D, E, keep, st);
     const unsigned blocks = unsigned((int64_t(rows) * (D.d / Elem<T>::VEC) + 255) / 256);
     LRSA_TIMED_LAUNCH("k_evict_rows", st, k_evict_rows<T>, dim3(blocks ? blocks : 1, 3, D.B * D.Hkv), dim3(256), 0, st, D, E, (const T*)K, (const T*)V,
                       keep, (T*)Ko, (T*)Vo);
@@ -226,8 +381,8 @@ hipError_t launch_cache_evict_quant(const Dims& D, const QuantDims& Q, const Qua
     const EvictArgs E = evict_args(D, lens, max_len, budget, recent, pos, acc, pos_o, acc_o, lens_o);
     int32_t* keep = (int32_t*)ws;
     const int rows = max_len < budget ? max_len : budget;
-    LRSA_TIMED_LAUNCH("k_evict_select", st, k_evict_select, dim3(D.B * D.Hkv), dim3(EVICT_THREADS), 0, st, D, E, keep);
-    const dim3 grid(unsigned((rows + N.block - 1) / N.block ? (rows + N.block - 1) / N.block : 1), 3, D.B * D.Hkv);
+    launch_select(D, E, keep, st);
+    const dim3 grid(unsigned(rows ? (rows + EVICT_WG_ROWS - 1) / EVICT_WG_ROWS : 1), 3, D.B * D.Hkv);
 #define LRSA_EVICT_QUANT(DH_, FMT_) LRSA_TIMED_LAUNCH("k_evict_quant", st, (k_evict_quant<DH_, FMT_>), grid, dim3(256), 0, st, D, E, Q, keep, N)
     if (Q.fmt == QUANT_INT8) {
         if (D.d == 64) LRSA_EVICT_QUANT(64, QUANT_INT8); else LRSA_EVICT_QUANT(128, QUANT_INT8);

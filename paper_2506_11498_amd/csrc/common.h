@@ -74,7 +74,7 @@ hipError_t launch_decode_attn_acc(const Dims&, const void* q, const void* Kc, co
                                   float* acc_out, float decay, void* ws, hipStream_t st);
 // eviction by accumulated weight
 size_t cache_evict_ws_bytes(const Dims&, int budget);
-bool cache_evict_grid_fits(const Dims&, int budget);
+bool cache_evict_grid_fits(const Dims&, int len, int budget);
 hipError_t launch_cache_evict(const Dims&, const void* K, const void* V, const int32_t* pos, const float* acc, int len, int budget, int recent,
                               void* Ko, void* Vo, int32_t* pos_o, float* acc_o, void* ws, hipStream_t st);
 // the cache in 8 bits

@@ -35,6 +35,13 @@ __device__ __forceinline__ float quant_scale(float top) {
     return __uint_as_float(uint32_t(e) << 23);
 }
 
+// Keeps the compiler from taking codes apart before they are used, or from keeping them so afterwards: as floats they take four times the
+// registers (k_decode_quant spilled, k_evict_quant ran two workgroups per CU).
+__device__ __forceinline__ uint32_t as_loaded(uint32_t w) {
+    asm("" : "+v"(w));
+    return w;
+}
+
 // 8 codes -> their whole or e4m3 numbers
 template <int FMT>
 __device__ __forceinline__ void code_values(uint2 c, float (&v)[8]) {
@@ -51,30 +58,44 @@ __device__ __forceinline__ void code_values(uint2 c, float (&v)[8]) {
         }
     }
 }
-// 8 values times `inv` -> codes; what lies beyond the largest code (only where the inputs are not finite) becomes that one
+// 8 values times `inv`, none beyond the largest code (but where inputs are not finite) -> codes
 template <int FMT>
 __device__ __forceinline__ uint2 make_codes(const float (&v)[8], float inv) {
-    constexpr float Q = FMT == QUANT_INT8 ? 127.0f : 448.0f;
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        float x[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = fminf(fmaxf(v[4 * i + j] * inv, -Q), Q);
         if constexpr (FMT == QUANT_INT8) {
-            w[i] = 0;
+            // 1.5 * 2^23 + x: numbers there are 1 apart, so the sum is rounded as wanted and its low byte is the code
+            uint32_t x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[i] |= (uint32_t(int(__builtin_rintf(x[j]))) & 255u) << (8 * j);
+            for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(__builtin_fmaf(v[4 * i + j], inv, 12582912.0f));
+            w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(x[3], x[2], 0x0c0c0400u), __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0400u), 0x05040100u);
         } else {
-            int c = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-            w[i] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], c, true));
+            int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] * inv, v[4 * i + 1] * inv, 0, false);
+            w[i] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] * inv, v[4 * i + 3] * inv, c, true));
         }
     }
     return uint2{w[0], w[1]};
 }
 
+// Reads and writes past the caches, of rows that are touched once
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 stream_load(const void* p) {
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    return uint4{v.x, v.y, v.z, v.w};
+}
+__device__ __forceinline__ void stream_store(void* p, const uint4& v) { __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p)); }
+
 // 8 neighbouring elements of a row
 __device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) { Elem<bf16_t>::load(p, v); }
+__device__ __forceinline__ void stream_load8(const bf16_t* p, float (&v)[8]) { Elem<bf16_t>::unpack(stream_load(p), v); }
+__device__ __forceinline__ void stream_load8(const float* p, float (&v)[8]) {
+    const uint4 a = stream_load(p), b = stream_load(p + 4);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
     const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
