@@ -109,22 +109,32 @@ struct QuantSlices {
 };
 struct QuantSeq { int base, n; };            // of one sequence: workgroup of its first slice, slices per KV head
 
+// The sequences' lengths, of the first 64 one per lane
+struct SeqLens {
+    const int32_t* lens;
+    int most, mine;
+    __device__ __forceinline__ SeqLens(const Dims& D, const int32_t* l, int max_len) : lens(l), most(max_len) {
+        const int lane = threadIdx.x & 63;
+        mine = lane < D.B ? seq_len(l, lane, max_len) : 0;
+    }
+    __device__ __forceinline__ int of(int b) const { return b < 64 ? __builtin_amdgcn_readlane(mine, b) : seq_len(lens, b, most); }
+};
 // wave-wide; `each` gets the tiles of the sequences in groups of 64, one per lane, until it returns true
 template <class Fn>
-__device__ __forceinline__ void each_sequence(const Dims& D, const int32_t* lens, int max_len, Fn each) {
+__device__ __forceinline__ void each_sequence(const Dims& D, const SeqLens& L, Fn each) {
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < D.B; b0 += 64) {
         const int b = b0 + lane;
-        if (each(b, b < D.B ? (seq_len(lens, b, max_len) + QT - 1) / QT : 0)) return;
+        if (each(b, ((b0 == 0 ? L.mine : b < D.B ? seq_len(L.lens, b, L.most) : 0) + QT - 1) / QT)) return;
     }
 }
 __device__ __forceinline__ int tiles_sum(int v) { return __builtin_amdgcn_readlane(wave_iscan(v), 63); }
-__device__ __forceinline__ int slice_tiles(const Dims& D, const int32_t* lens, int max_len, const QuantSlices& S) {
+__device__ __forceinline__ int slice_tiles(const Dims& D, const SeqLens& L, const QuantSlices& S) {
     int sum = 0, count = 0;
-    each_sequence(D, lens, max_len, [&](int, int t) { sum += t; return false; });
+    each_sequence(D, L, [&](int, int t) { sum += t; return false; });
     const float all = float(tiles_sum(sum));
     const int per = max(int(all * S.share) + 1, S.least);
-    each_sequence(D, lens, max_len, [&](int, int t) { count += (t + per - 1) / per; return false; });
+    each_sequence(D, L, [&](int, int t) { count += (t + per - 1) / per; return false; });
     return __builtin_amdgcn_readfirstlane(int64_t(tiles_sum(count)) * D.Hkv <= S.most ? per : max(int(all * S.safe) + 1, S.least));
 }
 
@@ -307,6 +317,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
     __shared__ float sM[DEC_WAVES][16], sL[DEC_WAVES][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q4 = lane >> 4;
     const int wg = blockIdx.x;
+    const SeqLens L(D, lens, max_len);
     int b = -1, h, r0, per;
     if (S.splits) {
         const int unit = wg / S.splits;
@@ -317,8 +328,8 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
     } else {
         // the sequence of this workgroup; the first workgroup notes all of them for the merge
         int first = 0, n = 1, before = 0;
-        per = slice_tiles(D, lens, max_len, S);
-        each_sequence(D, lens, max_len, [&](int bb, int t) {
+        per = slice_tiles(D, L, S);
+        each_sequence(D, L, [&](int bb, int t) {
             const int mine = (t + per - 1) / per, upto = before + D.Hkv * wave_iscan(mine);
             if (wg == 0 && wave == 0 && bb < D.B) seqs[bb] = QuantSeq{upto - D.Hkv * mine, mine};
             const uint64_t at = __builtin_amdgcn_ballot_w64(wg >= upto - D.Hkv * mine && wg < upto);
@@ -336,7 +347,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
         h = (wg - first) / n;
         r0 = (wg - first) % n * per * QT;
     }
-    const int bh = b * D.Hkv + h, len = seq_len(lens, b, max_len), r1 = min(len, r0 + per * QT);
+    const int bh = b * D.Hkv + h, len = L.of(b), r1 = min(len, r0 + per * QT);
     if (r0 >= r1) return;                                    // an empty slice: the merge does not ask for it
     const int64_t head = b * Q.st[0] + h * Q.st[1];
     const QuantRows R = {Q.K + head, Q.V + head, Q.Ks + int64_t(bh) * Q.nb, Q.Vs + int64_t(bh) * Q.nb, Q.st[2], Q.log_block};
@@ -411,8 +422,8 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
     }
 }
 
-// The first `rows` workgroups merge the slices of a query row each; the others, where weights are accumulated, take ACC_ROWS
-// cache rows of a unit each.
+// The first `rows` workgroups merge the slices of a query row each; the others, where weights are accumulated, take cache rows
+// of a unit.
 __device__ __forceinline__ void unit_slices(const Dims& D, const QuantSlices& S, const QuantSeq* seqs, int unit, int len, int& base, int& n) {
     if (S.splits) {
         base = unit * S.splits;
@@ -427,7 +438,7 @@ template <typename T>
 __global__ __launch_bounds__(DEC_THREADS) void k_quant_combine(Dims D, const float* __restrict__ part, int tokens, const int32_t* __restrict__ lens,
                                                                int max_len, QuantSlices S, const QuantSeq* __restrict__ seqs, T* __restrict__ O,
                                                                float* __restrict__ lse, AccArgs A, int rows, int chunks) {
-    __shared__ union { CombineLds c; float lse[ACC_COLS]; } sh;
+    __shared__ __attribute__((aligned(16))) union { CombineLds c; float lse[ACC_COLS]; } sh;
     const int rec = D.d + 2, cols = D.G * tokens;
     const int64_t step = int64_t(cols) * rec;
     int base, n;
@@ -437,7 +448,7 @@ __global__ __launch_bounds__(DEC_THREADS) void k_quant_combine(Dims D, const flo
         combine_row<T>(part + base * step + row % cols * rec, step, D.d, n, O + int64_t(row) * D.d, lse ? lse + row : nullptr, sh.c);
         return;
     }
-    const int at = int(blockIdx.x) - rows, unit = at / chunks, r0 = at % chunks * ACC_ROWS;
+    const int at = int(blockIdx.x) - rows, unit = at / chunks, r0 = at % chunks * acc_wg_rows(A.pitch);
     const int len = seq_len(lens, unit / D.Hkv, max_len);
     if (r0 >= len) return;
     unit_slices(D, S, seqs, unit, len, base, n);
@@ -519,7 +530,7 @@ static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
 size_t decode_quant_ws_bytes(const Dims& D, int tokens, int max_len, bool acc) { return quant_plan(D, tokens, max_len, acc).bytes; }
 // rows and tiles are counted in 32 bits
 bool decode_quant_grid_fits(const Dims& D, int tokens, int max_len) {
-    return max_len <= 1 << 30 && int64_t(D.B) * ((max_len + QT - 1) / QT) < int64_t(1) << 31 && grid_fits(int64_t(D.B) * D.Hq * tokens + int64_t(D.B) * D.Hkv * ((int64_t(max_len) + ACC_ROWS - 1) / ACC_ROWS), DEC_THREADS);
+    return max_len <= 1 << 30 && int64_t(D.B) * ((max_len + QT - 1) / QT) < int64_t(1) << 31 && grid_fits(int64_t(D.B) * D.Hq * tokens + int64_t(D.B) * D.Hkv * ((int64_t(max_len) + DEC_THREADS - 1) / DEC_THREADS), DEC_THREADS);
 }
 
 template <typename T>
@@ -530,7 +541,7 @@ static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void
     QuantSeq* seqs = reinterpret_cast<QuantSeq*>(w);
     float* part = reinterpret_cast<float*>(w + P.part);
     float* logits = acc_out ? reinterpret_cast<float*>(w + P.logits) : nullptr;
-    const int rows = D.B * D.Hq * tokens, chunks = acc_out ? (max_len - 1) / ACC_ROWS + 1 : 0;
+    const int rows = D.B * D.Hq * tokens, chunks = acc_out ? (max_len - 1) / acc_wg_rows(P.pitch) + 1 : 0;
     AccArgs A = {};
     A.logits = logits;
     A.mul = 1.0f;

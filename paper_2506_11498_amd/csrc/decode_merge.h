@@ -12,7 +12,6 @@ constexpr int DEC_THREADS = 256;
 constexpr int DEC_WAVES = DEC_THREADS / 64;
 constexpr int DEC_MAX_SPLITS = 256;
 constexpr int COMB_U = 4;
-constexpr int ACC_ROWS = 4 * DEC_THREADS;     // cache rows per workgroup of the weight sums
 
 // What the weight sums read besides the records: logits [unit][rows][pitch], in log2 units after the factor `mul`, -inf where
 // masked; a unit is one (sequence, KV head), its `cols` columns the query rows that read it, in the first cols of pitch values.
@@ -27,6 +26,8 @@ struct AccArgs {
     int64_t cap;
     float decay;
 };
+// cache rows per workgroup of the weight sums
+__host__ __device__ inline int acc_wg_rows(int pitch) { return DEC_THREADS * (pitch <= 8 ? 4 : pitch <= 16 ? 2 : 1); }
 
 #if defined(__HIPCC__)
 // A wave's logits on their way to memory.  They stay in LDS until it is full or the walk over the slice ends: a stream of reads that
@@ -99,6 +100,25 @@ __device__ __forceinline__ void merge_records(const float* src, int64_t step, in
     L = wave_sum(L);
 }
 
+// log2 of the whole weight of U query rows, `cols` floats apart, by a wave; +inf where there is none.  One record per lane: all rows'
+// records are asked for at once
+template <int U>
+__device__ __forceinline__ void merge_logs(const float* src, int64_t cols, int64_t step, int splits, float (&out)[U]) {
+    const int lane = threadIdx.x & 63;
+    float2 ml[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        ml[u] = float2{-INFINITY, 0.0f};
+        if (lane < splits) ml[u] = *reinterpret_cast<const float2*>(src + u * cols + lane * step);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const float M = wave_max(ml[u].x);
+        const float L = wave_sum(ml[u].x == -INFINITY ? 0.0f : ml[u].y * __builtin_amdgcn_exp2f(ml[u].x - M));
+        out[u] = L == 0.0f ? INFINITY : M + __builtin_log2f(L);
+    }
+}
+
 struct CombineLds {
     float w[DEC_MAX_SPLITS];
     float2 o[DEC_THREADS];
@@ -144,47 +164,77 @@ __device__ __forceinline__ void combine_row(const float* src, int64_t step, int 
     }
 }
 
-// acc_out[r] = decay acc_in[r] + sum over the columns of exp2(logit - log2 of the column's whole weight), for rows [r0, r0 +
-// ACC_ROWS) below `len`, by one workgroup; a row per thread, ACC_U rows at once.  `first`: record of the unit's first column,
-// columns `col_floats` apart.
+// acc_out[r] = decay acc_in[r] + sum over the columns of exp2(logit - log2 of the column's whole weight), for rows r0 .. below `len`, U
+// per thread, by one workgroup.  `first`: record of the unit's first column, columns `col_floats` apart.  Eight 16-byte reads of logits
+// per thread are on their way at once, the first ones while the columns' weights are put together.
 constexpr int ACC_COLS = 256;      // columns whose log-sum-exp is in LDS at once
-constexpr int ACC_U = ACC_ROWS / DEC_THREADS;
-__device__ __forceinline__ void acc_rows(const AccArgs& A, int unit, const float* first, int64_t col_floats, int64_t step, int splits, int r0, int len,
-                                         float* sLse) {
+template <int U>
+__device__ __forceinline__ void acc_rows_u(const AccArgs& A, int unit, const float* first, int64_t col_floats, int64_t step, int splits, int r0, int len,
+                                           float* sLse) {
+    constexpr int C = 8 / U;                 // groups of 4 columns at once
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float* s = A.logits + int64_t(unit) * A.rows * A.pitch;
-    float sum[ACC_U] = {};
+    const float* row[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) row[u] = s + int64_t(min(r0 + u * DEC_THREADS + tid, len - 1)) * A.pitch;
+    float4 x[C][U];
+    auto load = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[i][u] = *reinterpret_cast<const float4*>(row[u] + min(c0 + 4 * i, A.pitch - 4));
+    };
+    load(0);
+    float sum[U] = {};
     for (int c0 = 0; c0 < A.cols; c0 += ACC_COLS) {
         const int cn = min(ACC_COLS, A.cols - c0);
         if (c0) __syncthreads();
-        for (int c = wave; c < cn; c += DEC_WAVES) {
-            float w[DEC_MAX_SPLITS / 64], M, L;
-            merge_records(first + (c0 + c) * col_floats, step, splits, w, M, L);
-            if (lane == 0) sLse[c] = L == 0.0f ? INFINITY : M + __builtin_log2f(L);
+        // a wave takes a column, of many columns four at once
+        const int batch = cn > 8 && splits <= 64 ? 4 : 1;
+        for (int c = wave * batch; c < cn; c += DEC_WAVES * batch) {
+            if (c + batch <= cn && batch > 1) {
+                float logs[4];
+                merge_logs<4>(first + (c0 + c) * col_floats, col_floats, step, splits, logs);
+                if (lane == 0) *reinterpret_cast<float4*>(&sLse[c]) = float4{logs[0], logs[1], logs[2], logs[3]};
+                continue;
+            }
+            for (int k = c; k < min(c + batch, cn); ++k) {
+                float w[DEC_MAX_SPLITS / 64], M, L;
+                merge_records(first + (c0 + k) * col_floats, step, splits, w, M, L);
+                if (lane == 0) sLse[k] = L == 0.0f ? INFINITY : M + __builtin_log2f(L);
+            }
         }
         __syncthreads();
-        for (int c = 0; c < cn; c += 4) {
-            float4 x[ACC_U];
+        for (int cb = 0; cb < cn; cb += 4 * C) {
+            if (c0 + cb) load(c0 + cb);
 #pragma unroll
-            for (int u = 0; u < ACC_U; ++u)
-                x[u] = *reinterpret_cast<const float4*>(s + int64_t(min(r0 + u * DEC_THREADS + tid, len - 1)) * A.pitch + c0 + c);
-            const float4 n = *reinterpret_cast<const float4*>(&sLse[c]);
-            // a pad column's value is whatever was there
+            for (int i = 0; i < C; ++i) {
+                const int c = cb + 4 * i;
+                if (c >= cn) break;
+                const float4 n = *reinterpret_cast<const float4*>(&sLse[c]);
+                // a pad column's value is whatever was there
 #pragma unroll
-            for (int u = 0; u < ACC_U; ++u) {
-                sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].x, A.mul, -n.x));
-                if (c + 1 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].y, A.mul, -n.y));
-                if (c + 2 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].z, A.mul, -n.z));
-                if (c + 3 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u].w, A.mul, -n.w));
+                for (int u = 0; u < U; ++u) {
+                    sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][u].x, A.mul, -n.x));
+                    if (c + 1 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][u].y, A.mul, -n.y));
+                    if (c + 2 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][u].z, A.mul, -n.z));
+                    if (c + 3 < cn) sum[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][u].w, A.mul, -n.w));
+                }
             }
         }
     }
 #pragma unroll
-    for (int u = 0; u < ACC_U; ++u) {
+    for (int u = 0; u < U; ++u) {
         const int r = r0 + u * DEC_THREADS + tid;
         const int64_t at = int64_t(unit) * A.cap + r;
         if (r < len) A.out[at] = A.in ? __builtin_fmaf(A.decay, A.in[at], sum[u]) : sum[u];
     }
+}
+__device__ __forceinline__ void acc_rows(const AccArgs& A, int unit, const float* first, int64_t col_floats, int64_t step, int splits, int r0, int len,
+                                         float* sLse /* [ACC_COLS], 16-byte aligned */) {
+    if (A.pitch <= 8) acc_rows_u<4>(A, unit, first, col_floats, step, splits, r0, len, sLse);
+    else if (A.pitch <= 16) acc_rows_u<2>(A, unit, first, col_floats, step, splits, r0, len, sLse);
+    else acc_rows_u<1>(A, unit, first, col_floats, step, splits, r0, len, sLse);
 }
 #endif
 
