@@ -148,9 +148,11 @@ __device__ __forceinline__ int slice_tiles(const Dims& D, const SeqLens& L, cons
 // Codes have at most 8 significant bits, so both operands are exact in bf16 without their scales; the scale of K multiplies
 // the logit, that of V the weight, in fp32 (4 such rows share a block: blocks are multiples of 16).  Queries of fp32 enter as
 // three bf16 terms, which hold all 24 bits, and so do the weights.
-// Up to 16 columns: the 4 waves take the tiles in turn (SOLE), every code is read by one wave of the chip, past the caches.
-// More: `groups` (2 or 4) waves take the same tile, 16 columns each, so that its codes come from memory once; beyond 64
-// columns the slice is walked again.
+// A wave takes 16 * NG columns.  If these are all, the 4 waves take the tiles in turn (SOLE): every code is read by one wave of the
+// chip, past the caches.  Where there are more, `groups` (2 or 4) waves take the same tile, so that its codes come from memory once, and
+// beyond 4 times as many columns the slice is walked again.  NG = 2 halves the unpacking of codes, which bounds many columns (8 requests of
+// 32K rows, 20 columns: 107 us, with NG = 1 128; 64 columns: 171 and 212); it needs registers that fp32 queries of 128 channels do not
+// leave, and long walks.
 // The next tile's loads are in flight while a tile is used.  They are issued in every turn (the last one asks for its own tile
 // again, from the caches): loads in a branch make the compiler wait for all of them at its end, the next tile's too.
 constexpr float NO_WEIGHT = -1e30f;          // running maximum before the first visible row: finite, so that differences are
@@ -221,11 +223,13 @@ __device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantRow
     }
 }
 
-// seen: rows from the lane's first one on that its column sees; ACC: the logits go to `out`
-template <int DH, int FMT, int TERMS, bool ACC>
-__device__ __forceinline__ void use_quant_tile(float& m, float& l, f32x4 (&o)[DH / 16], const QuantTile<DH>& t, const bf16x8 (&qf)[TERMS][DH / 32],
-                                               int seen, float c2, LogitBuffer& out) {
-    f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+// NG groups of 16 columns.  seen: rows from the lane's first one on that its column sees; ACC: the logits go to `out`
+template <int DH, int FMT, int TERMS, bool ACC, int NG>
+__device__ __forceinline__ void use_quant_tile(float (&m)[NG], float (&l)[NG], f32x4 (&o)[NG][DH / 16], const QuantTile<DH>& t,
+                                               const bf16x8 (&qf)[NG][TERMS][DH / 32], const int (&seen)[NG], float c2, LogitBuffer (&out)[NG]) {
+    f32x4 s[NG][2];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) s[g][0] = s[g][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int kk = 0; kk < DH / 32; ++kk)
 #pragma unroll
@@ -236,41 +240,46 @@ __device__ __forceinline__ void use_quant_tile(float& m, float& l, f32x4 (&o)[DH
             codes_bf16<FMT>(as_loaded(kk % 2 ? w.w : w.y), a[2], a[3]);
             const bf16x8 kf = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
-            for (int i = TERMS - 1; i >= 0; --i) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][kk], s[kb], 0, 0, 0);
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int i = TERMS - 1; i >= 0; --i) s[g][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][i][kk], s[g][kb], 0, 0, 0);
         }
-    float p[8], mx = NO_WEIGHT;
     const float c2s[2] = {c2 * t.ks[0], c2 * t.ks[1]};
+    bf16x8 term[NG][3];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        p[j] = j % 4 + j / 4 * 16 < seen ? s[j >> 2][j & 3] * c2s[j >> 2] : -INFINITY;
-        mx = fmaxf(mx, p[j]);
-    }
-    if constexpr (ACC) keep_logits(out, p, [](int j) { return 4 * int(threadIdx.x >> 4 & 3) + j % 4 + j / 4 * 16; });
-    lanes_u32x2 x = pair32(__float_as_uint(mx));
-    mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
-    x = pair16(__float_as_uint(mx));
-    mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
-    if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
-        const float mn = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= a;
+    for (int g = 0; g < NG; ++g) {
+        float p[8], mx = NO_WEIGHT;
 #pragma unroll
-        for (int e = 0; e < DH / 16; ++e) o[e] *= a;
-    }
-    f32x8 w;
-    float ps = 0.0f;
+        for (int j = 0; j < 8; ++j) {
+            p[j] = j % 4 + j / 4 * 16 < seen[g] ? s[g][j >> 2][j & 3] * c2s[j >> 2] : -INFINITY;
+            mx = fmaxf(mx, p[j]);
+        }
+        if constexpr (ACC) keep_logits(out[g], p, [](int j) { return 4 * int(threadIdx.x >> 4 & 3) + j % 4 + j / 4 * 16; });
+        lanes_u32x2 x = pair32(__float_as_uint(mx));
+        mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
+        x = pair16(__float_as_uint(mx));
+        mx = fmaxf(__uint_as_float(x.x), __uint_as_float(x.y));
+        if (__builtin_amdgcn_ballot_w64(mx > m[g]) != 0) {
+            const float mn = fmaxf(m[g], mx), a = __builtin_amdgcn_exp2f(m[g] - mn);
+            m[g] = mn;
+            l[g] *= a;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float e = __builtin_amdgcn_exp2f(p[j] - m);
-        ps += e;
-        w[j] = e * t.vs[j >> 2];
-    }
-    l += ps;
-    bf16x8 term[3];
+            for (int e = 0; e < DH / 16; ++e) o[g][e] *= a;
+        }
+        f32x8 w;
+        float ps = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        term[i] = __builtin_convertvector(w, bf16x8);
-        w -= __builtin_convertvector(term[i], f32x8);
+        for (int j = 0; j < 8; ++j) {
+            const float e = __builtin_amdgcn_exp2f(p[j] - m[g]);
+            ps += e;
+            w[j] = e * t.vs[j >> 2];
+        }
+        l[g] += ps;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            term[g][i] = __builtin_convertvector(w, bf16x8);
+            w -= __builtin_convertvector(term[g][i], f32x8);
+        }
     }
 #pragma unroll
     for (int e0 = 0; e0 < DH / 16; e0 += 4) {
@@ -284,7 +293,9 @@ __device__ __forceinline__ void use_quant_tile(float& m, float& l, f32x4 (&o)[DH
             const uint32_t a[4] = {col[0][e], col[1][e], col[2][e], col[3][e]};
             const bf16x8 av = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
-            for (int i = 2; i >= 0; --i) o[e0 + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, term[i], o[e0 + e], 0, 0, 0);
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int i = 2; i >= 0; --i) o[g][e0 + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, term[g][i], o[g][e0 + e], 0, 0, 0);
         }
     }
 }
@@ -305,16 +316,16 @@ __device__ __forceinline__ void query_terms(const float* q, bf16x8 (&f)[3]) {
 }
 
 template <typename T> constexpr int Q_TERMS = sizeof(T) == 2 ? 1 : 3;
+template <typename T, int DH> constexpr int MOST_GROUPS = sizeof(T) == 2 || DH == 64 ? 2 : 1;      // NG
 
-template <typename T, int DH, int FMT, bool SOLE, bool ACC>
+template <typename T, int DH, int FMT, int NG, bool SOLE, bool ACC>
 __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDims Q, const T* __restrict__ q, int tokens, const int32_t* __restrict__ lens,
                                                                  int max_len, QuantSlices S, QuantSeq* __restrict__ seqs, float* __restrict__ part,
                                                                  float* __restrict__ logits, int64_t lrows, int pitch) {
-    constexpr int CPL = DH / 16, LROW = DH + 4, TERMS = Q_TERMS<T>, REC = DH + 2;
-    constexpr int WAVE_FLOATS = ACC ? LOGIT_FLOATS : 16 * LROW;      // a wave's logits, then its output
-    static_assert(WAVE_FLOATS >= 16 * LROW, "LDS of a wave");
+    constexpr int CPL = DH / 16, LROW = DH + 4, TERMS = Q_TERMS<T>, REC = DH + 2, CW = 16 * NG;       // CW: columns of a wave
+    constexpr int WAVE_FLOATS = ACC && LOGIT_FLOATS > CW * LROW ? LOGIT_FLOATS : CW * LROW;          // a wave's logits, then its output
     __shared__ __attribute__((aligned(16))) float sBuf[DEC_WAVES][WAVE_FLOATS];
-    __shared__ float sM[DEC_WAVES][16], sL[DEC_WAVES][16];
+    __shared__ float sM[DEC_WAVES][CW], sL[DEC_WAVES][CW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q4 = lane >> 4;
     const int wg = blockIdx.x;
     const SeqLens L(D, lens, max_len);
@@ -352,36 +363,52 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
     const int64_t head = b * Q.st[0] + h * Q.st[1];
     const QuantRows R = {Q.K + head, Q.V + head, Q.Ks + int64_t(bh) * Q.nb, Q.Vs + int64_t(bh) * Q.nb, Q.st[2], Q.log_block};
     const float c2 = D.scale * 1.4426950408889634f;          // logits in log2 units
-    const int cols = D.G * tokens, groups = SOLE ? 1 : cols <= 32 ? 2 : 4, ways = DEC_WAVES / groups;
+    const int cols = D.G * tokens, groups = SOLE ? 1 : cols <= 2 * CW ? 2 : 4, ways = DEC_WAVES / groups;
     const int64_t col0 = int64_t(bh) * cols;                 // query rows of the units before
 
-    for (int c0 = 0; c0 < cols; c0 += 16 * groups) {
-        const int g0 = c0 + 16 * (wave % groups), gn = min(16, cols - g0);      // of this wave: none where not positive
-        float m = NO_WEIGHT, l = 0.0f;
-        f32x4 o[CPL];
+    for (int c0 = 0; c0 < cols; c0 += CW * groups) {
+        const int g0 = c0 + CW * (wave % groups), gn = min(CW, cols - g0);      // of this wave: none where not positive
+        float m[NG], l[NG];
+        f32x4 o[NG][CPL];
 #pragma unroll
-        for (int e = 0; e < CPL; ++e) o[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int g = 0; g < NG; ++g) {
+            m[g] = NO_WEIGHT;
+            l[g] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) o[g][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
         const int step = ways * QT;
         int r = r0 + wave / groups * QT;
         if (gn > 0 && r < r1) {
-            const int col = g0 + min(c, gn - 1);
-            const int vis = len - tokens + 1 + col % tokens;     // rows that the column sees, none where that is not positive
-            const T* qrow = q + (col0 + col) * DH;
             const int end = r + (r1 - 1 - r) / step * step;      // the wave's last tile
             auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, SOLE>(t, R, min(row, end), q4, c, r1 - 1); };
             QuantTile<DH> A, B;
             load(A, r);
-            bf16x8 qf[TERMS][DH / 32];
+            bf16x8 qf[NG][TERMS][DH / 32];
+            int vis[NG];                                         // rows that the column sees, none where that is not positive
+            LogitBuffer out[NG] = {};
 #pragma unroll
-            for (int kk = 0; kk < DH / 32; ++kk) {
-                bf16x8 f[TERMS];
-                query_terms(qrow + (kk / 2) * 64 + q4 * 16 + (kk % 2) * 8, f);
+            for (int g = 0; g < NG; ++g) {
+                const int col = g0 + min(16 * g + c, gn - 1);
+                vis[g] = min(r1, len - tokens + 1 + col % tokens) - 4 * q4;
+                const T* qrow = q + (col0 + col) * DH;
 #pragma unroll
-                for (int i = 0; i < TERMS; ++i) qf[i][kk] = f[i];
+                for (int kk = 0; kk < DH / 32; ++kk) {
+                    bf16x8 f[TERMS];
+                    query_terms(qrow + (kk / 2) * 64 + q4 * 16 + (kk % 2) * 8, f);
+#pragma unroll
+                    for (int i = 0; i < TERMS; ++i) qf[g][i][kk] = f[i];
+                }
+                if constexpr (ACC)
+                    out[g] = logit_buffer(sBuf[wave] + g * (LOGIT_FLOATS / NG), LOGIT_FLOATS / NG,
+                                          logits + (int64_t(bh) * lrows + r) * pitch + g0 + 16 * g, pitch, max(0, min(16, gn - 16 * g)), step);
             }
-            LogitBuffer out = {};
-            if constexpr (ACC) out = logit_buffer(sBuf[wave], logits + (int64_t(bh) * lrows + r) * pitch + g0, pitch, gn, step);
-            auto use = [&](const QuantTile<DH>& t) { use_quant_tile<DH, FMT, TERMS, ACC>(m, l, o, t, qf, min(r1, vis) - r - 4 * q4, c2, out); };
+            auto use = [&](const QuantTile<DH>& t) {
+                int seen[NG];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) seen[g] = vis[g] - r;
+                use_quant_tile<DH, FMT, TERMS, ACC, NG>(m, l, o, t, qf, seen, c2, out);
+            };
             for (;;) {
                 load(B, r + step);
                 use(A);
@@ -390,24 +417,31 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
                 use(B);
                 if ((r += step) >= r1) break;
             }
-            if constexpr (ACC) flush_logits(out);
+            if constexpr (ACC)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) flush_logits(out[g]);
         }
-        lanes_u32x2 x = pair32(__float_as_uint(l));
-        l = __uint_as_float(x.x) + __uint_as_float(x.y);
-        x = pair16(__float_as_uint(l));
-        l = __uint_as_float(x.x) + __uint_as_float(x.y);
-        if (c < gn) {
-            if (q4 == 0) { sM[wave][c] = m; sL[wave][c] = l; }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int g = 0; g < NG; ++g) {
+            lanes_u32x2 x = pair32(__float_as_uint(l[g]));
+            l[g] = __uint_as_float(x.x) + __uint_as_float(x.y);
+            x = pair16(__float_as_uint(l[g]));
+            l[g] = __uint_as_float(x.x) + __uint_as_float(x.y);
+            const int cw = 16 * g + c;
+            if (cw < gn) {
+                if (q4 == 0) { sM[wave][cw] = m[g]; sL[wave][cw] = l[g]; }
 #pragma unroll
-                for (int e = 0; e < CPL; e += 4)
-                    *reinterpret_cast<f32x4*>(&sBuf[wave][c * LROW + (4 * q4 + i) * CPL + e]) = f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < CPL; e += 4)
+                        *reinterpret_cast<f32x4*>(&sBuf[wave][cw * LROW + (4 * q4 + i) * CPL + e]) =
+                            f32x4{o[g][e][i], o[g][e + 1][i], o[g][e + 2][i], o[g][e + 3][i]};
+            }
         }
         __syncthreads();
-        // column g of the walk is in the waves g / 16, + groups, ...
-        for (int e = tid; e < min(16 * groups, cols - c0) * DH; e += DEC_THREADS) {
-            const int g = e / DH, ch = e % DH, w0 = g >> 4, gc = g & 15;
+        // column g of the walk is in the waves g / CW, + groups, ...
+        for (int e = tid; e < min(CW * groups, cols - c0) * DH; e += DEC_THREADS) {
+            const int g = e / DH, ch = e % DH, w0 = g / CW, gc = g % CW;
             float mm = sM[w0][gc], ll = sL[w0][gc], oo = sBuf[w0][gc * LROW + ch];
             for (int w = w0 + groups; w < DEC_WAVES; w += groups) {
                 float a, b2;
@@ -500,8 +534,13 @@ hipError_t launch_read_quant(const Dims& D, const QuantDims& Q, const int32_t* l
     return D.dtype == 1 ? run_read<bf16_t>(D, Q, lens, rows, first, K, V, st) : run_read<float>(D, Q, lens, rows, first, K, V, st);
 }
 
+// Tiles of a slice from which on a wave takes two groups of columns.  Shorter walks are bound by their latency, of which two groups have
+// more.  8 requests on 8 KV heads of 4 query heads, 16 tokens each, bf16, d 128, one group and two: 4K rows (16 tiles) 39.0 and 40.1 us,
+// 8K 60.6 and 56.7, 16K (62) 98.4 and 87.5; 8 tokens: 26.2 and 31.4, 38.8 and 41.8, 61.9 and 58.0; d 64: 18.9 and 21.4, 26.1 and 28.4,
+// 39.7 and 39.5.
+constexpr int WIDE_TILES = 40;
 namespace {
-struct QuantPlan { QuantSlices s; int grid, pitch; int64_t rows; size_t part, logits, bytes; };
+struct QuantPlan { QuantSlices s; int grid, pitch; bool wide; int64_t rows; size_t part, logits, bytes; };
 }
 // Workspace: a QuantSeq per sequence, the records of `grid` workgroups, the logits.  All of them grow with max_len.
 static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
@@ -519,6 +558,7 @@ static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
     if (P.s.least < DEC_WAVES) P.s.least = DEC_WAVES;          // a tile per wave
     P.grid = int(most < fine ? most : fine);
     if (fine <= most && P.s.least == DEC_WAVES) P.s.splits = int(fine / units);
+    P.wide = units * tiles >= most * WIDE_TILES;
     P.rows = tiles * QT;
     const size_t cols = size_t(D.G) * tokens;
     P.part = align256(size_t(D.B) * sizeof(QuantSeq));
@@ -552,16 +592,26 @@ static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void
     A.out = acc_out;
     A.cap = D.n;
     A.decay = decay;
-#define LRSA_DECODE_QUANT(DH_, FMT_, SOLE_)                                                                                              \
-    LRSA_TIMED_LAUNCH("k_decode_quant", st, (acc_out ? k_decode_quant<T, DH_, FMT_, SOLE_, true> : k_decode_quant<T, DH_, FMT_, SOLE_, false>), dim3(P.grid), dim3(DEC_THREADS), 0, st, D, Q,          \
-                      (const T*)q, tokens, lens, max_len, P.s, seqs, part, logits, P.rows, P.pitch)
-#define LRSA_DECODE_QUANT_FMT(DH_, FMT_) \
-    if (A.cols <= 16) LRSA_DECODE_QUANT(DH_, FMT_, true); else LRSA_DECODE_QUANT(DH_, FMT_, false)
-    if (Q.fmt == QUANT_INT8) {
-        if (D.d == 64) { LRSA_DECODE_QUANT_FMT(64, QUANT_INT8); } else { LRSA_DECODE_QUANT_FMT(128, QUANT_INT8); }
-    } else {
-        if (D.d == 64) { LRSA_DECODE_QUANT_FMT(64, QUANT_E4M3); } else { LRSA_DECODE_QUANT_FMT(128, QUANT_E4M3); }
+#define LRSA_DECODE_QUANT(DH_, FMT_, NG_, SOLE_)                                                                                          \
+    LRSA_TIMED_LAUNCH("k_decode_quant", st,                                                                                               \
+                      (acc_out ? k_decode_quant<T, DH_, FMT_, NG_, SOLE_, true> : k_decode_quant<T, DH_, FMT_, NG_, SOLE_, false>),        \
+                      dim3(P.grid), dim3(DEC_THREADS), 0, st, D, Q, (const T*)q, tokens, lens, max_len, P.s, seqs, part, logits, P.rows,   \
+                      P.pitch)
+#define LRSA_DECODE_QUANT_FMT(DH_, FMT_)                                                            \
+    if (A.cols <= 16) LRSA_DECODE_QUANT(DH_, FMT_, 1, true);                                        \
+    else if (!P.wide) LRSA_DECODE_QUANT(DH_, FMT_, 1, false);                                       \
+    else if (A.cols <= 16 * MOST) LRSA_DECODE_QUANT(DH_, FMT_, MOST, true);                         \
+    else LRSA_DECODE_QUANT(DH_, FMT_, MOST, false)
+#define LRSA_DECODE_QUANT_DH(FMT_)                                                                  \
+    if (D.d == 64) {                                                                                \
+        constexpr int MOST = MOST_GROUPS<T, 64>;                                                    \
+        LRSA_DECODE_QUANT_FMT(64, FMT_);                                                            \
+    } else {                                                                                        \
+        constexpr int MOST = MOST_GROUPS<T, 128>;                                                   \
+        LRSA_DECODE_QUANT_FMT(128, FMT_);                                                           \
     }
+    if (Q.fmt == QUANT_INT8) { LRSA_DECODE_QUANT_DH(QUANT_INT8) } else { LRSA_DECODE_QUANT_DH(QUANT_E4M3) }
+#undef LRSA_DECODE_QUANT_DH
 #undef LRSA_DECODE_QUANT_FMT
 #undef LRSA_DECODE_QUANT
     LRSA_TIMED_LAUNCH("k_quant_combine", st, k_quant_combine<T>, dim3(unsigned(rows + D.B * D.Hkv * chunks)), dim3(DEC_THREADS), 0, st, D, part, tokens,

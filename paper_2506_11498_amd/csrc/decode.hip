@@ -458,7 +458,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
         constexpr int STEP = DEC_WAVES * DEC_TILE;
         int r = r0 + wave * DEC_TILE;
         LogitBuffer out = {};      // tiles begin at multiples of 32 rows, and so does the end of the rows that there is room for
-        if constexpr (LOGITS) out = logit_buffer(sBuf[wave], logits + (int64_t(bh) * lrows + r) * pitch + g0, pitch, gn, STEP);
+        if constexpr (LOGITS) out = logit_buffer(sBuf[wave], LOGIT_FLOATS, logits + (int64_t(bh) * lrows + r) * pitch + g0, pitch, gn, STEP);
         if (r < r1) {
             DecTile<DH> A, B;
             const int end = r + (r1 - 1 - r) / STEP * STEP;      // the wave's last tile

@@ -40,9 +40,10 @@ struct LogitBuffer {
     int pitch, gn, used, most;
     int64_t skip;            // floats between tiles in memory
 };
-__device__ __forceinline__ LogitBuffer logit_buffer(float* lds, float* dst, int pitch, int gn, int step) {
+// lds: `floats` of it; gn columns, none where 0
+__device__ __forceinline__ LogitBuffer logit_buffer(float* lds, int floats, float* dst, int pitch, int gn, int step) {
     const int width = (gn + 3) & ~3;
-    return LogitBuffer{lds, dst, pitch, gn, 0, LOGIT_FLOATS / (32 * width), int64_t(step) * pitch};
+    return LogitBuffer{lds, dst, pitch, gn, 0, floats / (32 * max(width, 4)), int64_t(step) * pitch};
 }
 __device__ __forceinline__ void flush_logits(LogitBuffer& B) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
