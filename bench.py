@@ -41,7 +41,7 @@ STAGES = {
     "cache_compress": ("k_cache_compress", "k_cache_select_move", "k_cache_gather", "k_cache_place"),
     "cache_evict": ("k_evict_select", "k_evict_rows", "k_evict_quant"),
     "cache_quant": ("k_append_quant", "k_read_quant"),
-    "decode_attn_quant": ("k_decode_quant", "k_quant_combine"),
+    "decode_attn_quant": ("k_decode_quant", "k_decode_quant_short", "k_quant_combine"),
 }
 
 

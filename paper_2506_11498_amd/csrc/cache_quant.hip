@@ -5,6 +5,7 @@
 // k_append_quant      new rows into the blocks of the cache that they belong to
 // k_read_quant        rows of the cache as values
 // k_decode_quant      attention of the query rows of a KV group over a slice of the cache rows, on the matrix cores
+// k_decode_quant_short  the same over whole short caches, with everything that follows, in one launch
 // k_quant_combine     merges the slices; with accumulated weights the same workgroup kinds as k_decode_combine_acc
 #include "decode_merge.h"
 #include "mfma_tiles.h"
@@ -456,6 +457,105 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
     }
 }
 
+// Short caches (SHORT_ROWS rows at most, 16 columns): one workgroup per unit, whose 8 waves take all tiles, merge, and write O, lse and
+// the accumulated weights.  A call is one launch, which bounds it (8.4 us, 12 with slices and their merge, call after call: 1 request
+// of 777 rows, 12 heads of 64 on 2); but a unit's rows pass through one CU, where slices would spread few units over many.  See
+// short_cache for where that costs more than the launch.
+constexpr int SHORT_WAVES = 8, SHORT_TILES = 4, SHORT_ROWS = SHORT_WAVES * SHORT_TILES * QT;
+template <typename T, int DH, int FMT, bool ACC>
+__global__ __launch_bounds__(64 * SHORT_WAVES) void k_decode_quant_short(Dims D, QuantDims Q, const T* __restrict__ q, int tokens,
+                                                                         const int32_t* __restrict__ lens, int max_len, T* __restrict__ O,
+                                                                         float* __restrict__ lse, AccArgs A) {
+    constexpr int CPL = DH / 16, LROW = DH + 4, TERMS = Q_TERMS<T>, THREADS = 64 * SHORT_WAVES, LOGITS = SHORT_TILES * QT * 16;
+    __shared__ __attribute__((aligned(16))) float sO[SHORT_WAVES][16 * LROW];
+    __shared__ __attribute__((aligned(16))) float sLogit[ACC ? SHORT_WAVES : 1][ACC ? LOGITS : 1];
+    __shared__ float sM[SHORT_WAVES][16], sL[SHORT_WAVES][16], sLse[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q4 = lane >> 4;
+    const int bh = blockIdx.x, b = bh / D.Hkv, h = bh % D.Hkv, len = seq_len(lens, b, max_len);
+    const int64_t head = b * Q.st[0] + h * Q.st[1];
+    const QuantRows R = {Q.K + head, Q.V + head, Q.Ks + int64_t(bh) * Q.nb, Q.Vs + int64_t(bh) * Q.nb, Q.st[2], Q.log_block};
+    const float c2 = D.scale * 1.4426950408889634f;
+    const int cols = D.G * tokens, width = (cols + 3) & ~3;
+    const int64_t col0 = int64_t(bh) * cols;
+    float m[1] = {NO_WEIGHT}, l[1] = {0.0f};
+    f32x4 o[1][CPL];
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) o[0][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    int r = wave * QT;
+    if (r < len) {
+        constexpr int STEP = SHORT_WAVES * QT;
+        const int end = r + (len - 1 - r) / STEP * STEP, col = min(c, cols - 1);
+        auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, true>(t, R, min(row, end), q4, c, len - 1); };
+        QuantTile<DH> A0, B0;
+        load(A0, r);
+        bf16x8 qf[1][TERMS][DH / 32];
+        const T* qrow = q + (col0 + col) * DH;
+#pragma unroll
+        for (int kk = 0; kk < DH / 32; ++kk) {
+            bf16x8 f[TERMS];
+            query_terms(qrow + (kk / 2) * 64 + q4 * 16 + (kk % 2) * 8, f);
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i) qf[0][i][kk] = f[i];
+        }
+        const int vis = min(len, len - tokens + 1 + col % tokens) - 4 * q4;
+        LogitBuffer out[1] = {};
+        if constexpr (ACC) out[0] = logit_buffer(sLogit[wave], LOGITS, nullptr, 0, cols, 0);      // room for all of the wave's tiles
+        auto use = [&](const QuantTile<DH>& t) {
+            const int seen[1] = {vis - r};
+            use_quant_tile<DH, FMT, TERMS, ACC, 1>(m, l, o, t, qf, seen, c2, out);
+        };
+        for (;;) {
+            load(B0, r + STEP);
+            use(A0);
+            if ((r += STEP) >= len) break;
+            load(A0, r + STEP);
+            use(B0);
+            if ((r += STEP) >= len) break;
+        }
+    }
+    lanes_u32x2 x = pair32(__float_as_uint(l[0]));
+    l[0] = __uint_as_float(x.x) + __uint_as_float(x.y);
+    x = pair16(__float_as_uint(l[0]));
+    l[0] = __uint_as_float(x.x) + __uint_as_float(x.y);
+    if (c < cols) {
+        if (q4 == 0) { sM[wave][c] = m[0]; sL[wave][c] = l[0]; }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < CPL; e += 4)
+                *reinterpret_cast<f32x4*>(&sO[wave][c * LROW + (4 * q4 + i) * CPL + e]) = f32x4{o[0][e][i], o[0][e + 1][i], o[0][e + 2][i], o[0][e + 3][i]};
+    }
+    __syncthreads();
+    const int waves = max(1, min(SHORT_WAVES, (len + QT - 1) / QT));         // those that had a tile
+    for (int e = tid; e < cols * DH; e += THREADS) {
+        const int g = e / DH, ch = e % DH;
+        float M = sM[0][g], sum = 0.0f, val = 0.0f;
+        for (int w = 1; w < waves; ++w) M = fmaxf(M, sM[w][g]);
+        for (int w = 0; w < waves; ++w) {
+            const float a = __builtin_amdgcn_exp2f(sM[w][g] - M);
+            sum = __builtin_fmaf(sL[w][g], a, sum);
+            val = __builtin_fmaf(sO[w][g * LROW + ch], a, val);
+        }
+        const bool none = sum == 0.0f;
+        Elem<T>::put(O + (col0 + g) * DH + ch, none ? 0.0f : val / sum);
+        if (ch == 0) {
+            sLse[g] = none ? INFINITY : M + __builtin_log2f(sum);
+            if (lse) lse[col0 + g] = none ? -INFINITY : log2_to_ln(M, sum);
+        }
+    }
+    if constexpr (ACC) {
+        __syncthreads();
+        for (int i = tid; i < len; i += THREADS) {
+            const int tile = i / QT;
+            const float* p = sLogit[tile % SHORT_WAVES] + (tile / SHORT_WAVES * QT + i % QT) * width;
+            float t = 0.0f;
+            for (int g = 0; g < cols; ++g) t += __builtin_amdgcn_exp2f(p[g] - sLse[g]);
+            const int64_t at = int64_t(bh) * A.cap + i;
+            A.out[at] = A.in ? __builtin_fmaf(A.decay, A.in[at], t) : t;
+        }
+    }
+}
+
 // The first `rows` workgroups merge the slices of a query row each; the others, where weights are accumulated, take cache rows
 // of a unit.
 __device__ __forceinline__ void unit_slices(const Dims& D, const QuantSlices& S, const QuantSeq* seqs, int unit, int len, int& base, int& n) {
@@ -546,9 +646,10 @@ struct QuantPlan { QuantSlices s; int grid, pitch; bool wide; int64_t rows; size
 static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
     QuantPlan P = {};
     const int64_t units = int64_t(D.B) * D.Hkv;
-    // two workgroups share a CU (registers), so 512 run at once; with so many units that some of these would have two slices and some one,
-    // several rounds
-    const int64_t most = units <= 256 ? 512 : units + 2048;
+    // Two workgroups share a CU (registers), so 512 run at once.  With more units than half of that some would have two slices and some
+    // one: then several rounds, of few more slices than units.  8 KV heads, 64 requests of 2048 rows: units + 256 55 us, + 512 58,
+    // + 768 67, + 2048 71; 33 of 4096: 80, 70, 65, 70.
+    const int64_t most = units <= 256 ? 512 : units + 512;
     const int64_t tiles = (int64_t(max_len) + QT - 1) / QT, fine = units * ((tiles + DEC_WAVES - 1) / DEC_WAVES);
     const float up = 1.0f + 0x1p-20f;
     P.s.most = int(most);
@@ -573,6 +674,13 @@ bool decode_quant_grid_fits(const Dims& D, int tokens, int max_len) {
     return max_len <= 1 << 30 && int64_t(D.B) * ((max_len + QT - 1) / QT) < int64_t(1) << 31 && grid_fits(int64_t(D.B) * D.Hq * tokens + int64_t(D.B) * D.Hkv * ((int64_t(max_len) + DEC_THREADS - 1) / DEC_THREADS), DEC_THREADS);
 }
 
+// One workgroup per unit, or slices?  Heads of 64: one, always (1 request of 1024 rows 8.8 us, slices 12.0; 64 of 1024 16.7, 30.3).
+// Heads of 128 have twice the bytes: one where it is short (12 heads on 2, 100 rows: 8.7, 12.5) or where units fill the card (16 requests of 1000 rows: 15.9, 17.5; 64 of 1024: 31.9, 51.3), slices else (1 request of
+// 1024 rows: 13.8, 12.0).
+static bool short_cache(const Dims& D, int cols, int max_len) {
+    return cols <= 16 && max_len <= SHORT_ROWS && (D.d == 64 || max_len <= SHORT_ROWS / 2 || int64_t(D.B) * D.Hkv >= 128);
+}
+
 template <typename T>
 static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void* q, int tokens, const int32_t* lens, int max_len, void* O, float* lse,
                                    const float* acc_in, float* acc_out, float decay, void* ws, hipStream_t st) {
@@ -592,6 +700,19 @@ static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void
     A.out = acc_out;
     A.cap = D.n;
     A.decay = decay;
+    if (short_cache(D, A.cols, max_len)) {
+#define LRSA_DECODE_SHORT(DH_, FMT_)                                                                                                      \
+    LRSA_TIMED_LAUNCH("k_decode_quant_short", st,                                                                                         \
+                      (acc_out ? k_decode_quant_short<T, DH_, FMT_, true> : k_decode_quant_short<T, DH_, FMT_, false>),                    \
+                      dim3(D.B * D.Hkv), dim3(64 * SHORT_WAVES), 0, st, D, Q, (const T*)q, tokens, lens, max_len, (T*)O, lse, A)
+        if (Q.fmt == QUANT_INT8) {
+            if (D.d == 64) LRSA_DECODE_SHORT(64, QUANT_INT8); else LRSA_DECODE_SHORT(128, QUANT_INT8);
+        } else {
+            if (D.d == 64) LRSA_DECODE_SHORT(64, QUANT_E4M3); else LRSA_DECODE_SHORT(128, QUANT_E4M3);
+        }
+#undef LRSA_DECODE_SHORT
+        return hipGetLastError();
+    }
 #define LRSA_DECODE_QUANT(DH_, FMT_, NG_, SOLE_)                                                                                          \
     LRSA_TIMED_LAUNCH("k_decode_quant", st,                                                                                               \
                       (acc_out ? k_decode_quant<T, DH_, FMT_, NG_, SOLE_, true> : k_decode_quant<T, DH_, FMT_, NG_, SOLE_, false>),        \

@@ -120,6 +120,11 @@ __device__ __forceinline__ void merge_logs(const float* src, int64_t cols, int64
     }
 }
 
+// natural log of 2^M * L.  One rounding at the end: ln 2 as its fp32 value plus the rest
+__device__ __forceinline__ float log2_to_ln(float M, float L) {
+    return __builtin_fmaf(M, 0.69314718246459961f, __builtin_fmaf(M, -1.9046542e-9f, __builtin_log2f(L) * 0.6931471805599453f));
+}
+
 struct CombineLds {
     float w[DEC_MAX_SPLITS];
     float2 o[DEC_THREADS];
@@ -160,8 +165,7 @@ __device__ __forceinline__ void combine_row(const float* src, int64_t step, int 
         const bool none = L == 0.0f;
         Elem<T>::put(O + 2 * ch, none ? 0.0f : o.x / L);
         Elem<T>::put(O + 2 * ch + 1, none ? 0.0f : o.y / L);
-        if (lse && tid == 0)   // one rounding at the end: ln 2 as its fp32 value plus the rest
-            *lse = none ? -INFINITY : __builtin_fmaf(M, 0.69314718246459961f, __builtin_fmaf(M, -1.9046542e-9f, __builtin_log2f(L) * 0.6931471805599453f));
+        if (lse && tid == 0) *lse = none ? -INFINITY : log2_to_ln(M, L);
     }
 }
 

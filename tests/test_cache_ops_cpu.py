@@ -148,6 +148,7 @@ def test_quant_calls_refuse():
     each(_c(Vs=ctypes.c_void_p((1 << 16) + 2)), -1, "4-byte")
     for st in ((25600, 12800, 64), (25600, 12800, 136), (25608, 12800, 128), (-25600, 12800, 128)):
         each(_c(stride=st), -1, "stride")
+    each(_c(stride=(1 << 34, 128, 1 << 24)), -2, "apart")
 
     c = ctypes.byref(_c())
     for kw in ((None, FAKE, 1, FAKE), (FAKE, None, 1, FAKE), (FAKE, FAKE, 1, None)):
