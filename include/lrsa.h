@@ -312,7 +312,8 @@ int lrsa_cache_evict(const lrsa_params *p, const void *Kc, const void *Vc, const
  * A row's value is code * scale of its block.  The scale is a power of two: the least 2^e, e >= -120, by which the block's
  * largest magnitude does not exceed the largest code (int8: 127, e4m3: 448); the code is the nearest one to value / scale, ties
  * to even.  Values are then exact in bf16, and rows that change their block keep their value unless the new block's scale is
- * too coarse for it.  (The attention call takes any finite scales with which the logits stay below 1e29, and int8 codes down to -128.)
+ * too coarse for it.  A row that holds NaN or infinities gives its block an unspecified finite scale and finite codes; other
+ * blocks do not change.  (The attention call takes any finite scales with which the logits stay below 1e29, and int8 codes down to -128.)
  *
  * In these calls p->seq is cap, the rows that the cache has room for; dtype is that of q, O and of the rows K, V given to
  * lrsa_cache_append_quant and taken by lrsa_cache_read_quant, which kv_stride describes; q_stride is not used.  Every sequence

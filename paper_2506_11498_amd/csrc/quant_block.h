@@ -58,7 +58,8 @@ __device__ __forceinline__ void code_values(uint2 c, float (&v)[8]) {
         }
     }
 }
-// 8 values times `inv`, none beyond the largest code (but where inputs are not finite) -> codes
+// 8 values times `inv`, none beyond the largest code -> codes.  What is infinite or no number gets some finite code (int8 by what the
+// sum's low byte is, e4m3 by the clamp): a row that a token does not see then has no part in its output, 0 * code being 0.
 template <int FMT>
 __device__ __forceinline__ uint2 make_codes(const float (&v)[8], float inv) {
     uint32_t w[2];
@@ -71,8 +72,11 @@ __device__ __forceinline__ uint2 make_codes(const float (&v)[8], float inv) {
             for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(__builtin_fmaf(v[4 * i + j], inv, 12582912.0f));
             w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(x[3], x[2], 0x0c0c0400u), __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0400u), 0x05040100u);
         } else {
-            int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] * inv, v[4 * i + 1] * inv, 0, false);
-            w[i] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] * inv, v[4 * i + 3] * inv, c, true));
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_fmed3f(v[4 * i + j] * inv, -448.0f, 448.0f);
+            const int c = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+            w[i] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], c, true));
         }
     }
     return uint2{w[0], w[1]};

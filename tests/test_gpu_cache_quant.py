@@ -135,6 +135,30 @@ def test_rows_that_are_no_numbers_leave_the_other_blocks_alone():
     assert np.array_equal(a[2][0, 0, [0, 2, 3]], b[2][0, 0, [0, 2, 3]])
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,block", [(64, 16), (2048, 64)])
+def test_tokens_do_not_see_later_rows_that_are_no_numbers(fmt, dtype, n, block):
+    """The last of three tokens has rows of NaN and infinities, in a block of its own: the others' outputs keep their bits, and no
+    code or scale becomes one that is no number."""
+    d, T = 128, DT[dtype]
+    g = torch.Generator().manual_seed(n)
+    x, q = torch.randn((1, 1, n + 1, d), generator=g).to(T), torch.randn((1, 4, 3, d), generator=g).to(T).to(DEV)
+    outs = []
+    for bad in (False, True):
+        cache = lrsa.QuantCache.empty(1, 1, n + 70, d, CODES[fmt], block, DEV)
+        if bad:
+            x[0, 0, n, ::3], x[0, 0, n, 1::3], x[0, 0, n, 2::7] = float("nan"), float("inf"), -float("inf")
+        p = params(1, 4, 1, n + 70, d, x.stride(), T)
+        lrsa.lrsa_cache_append_quant(p, cache, x.to(DEV), x.to(DEV), i32([0]))
+        O, lse = lrsa.lrsa_decode_attn_quant(p, q, cache, i32([n + 1]), n + 70)
+        K, V, Ks, Vs = host(cache)
+        j = n // block
+        assert np.all(np.isfinite(ops.values(V[0, 0, :n + 1], Vs[0, 0, :j + 1], block, fmt) / Vs[0, 0, j])) and np.isfinite(Ks[0, 0, j])
+        outs.append((O[:, :, :2].clone(), lse[:, :, :2].clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
 # ------------------------------------------------------------------------------------------------ attention
 def check_attention(p, cache, q, lens, max_len, acc=None, decay=1.0, fmt="int8", dtype="bf16", scale=None):
     B, Hq, T, d = q.shape
