@@ -39,7 +39,7 @@ STAGES = {
                  "k_bwd_dkv_genericT", "k_bwd_scatter_dkv", "k_bwd_acc_finish", "k_compact_kv"),   # k_compact_kv runs in both calls
     "decode_attn": ("k_decode_mfma", "k_decode_attn", "k_decode_combine", "k_decode_combine_acc"),
     "cache_compress": ("k_cache_compress", "k_cache_select_move", "k_cache_gather", "k_cache_place"),
-    "cache_evict": ("k_evict_select", "k_evict_rows", "k_evict_quant"),
+    "cache_evict": ("k_evict_select", "k_evict_rows", "k_evict_quant", "k_evict_short", "k_evict_quant_short"),
     "cache_quant": ("k_append_quant", "k_read_quant"),
     "decode_attn_quant": ("k_decode_quant", "k_decode_quant_short", "k_quant_combine"),
 }

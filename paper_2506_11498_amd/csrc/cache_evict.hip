@@ -6,6 +6,7 @@
 // k_evict_select    one workgroup per (sequence, KV head): the list of rows that stay
 // k_evict_rows      fp32 and bf16 caches: rows, positions and weights by that list
 // k_evict_quant     8-bit caches: the same, in blocks with a scale of their own
+// k_evict_short, k_evict_quant_short  both steps in one launch, for short caches
 #include "quant_block.h"
 #include "select_block.h"
 
@@ -42,20 +43,18 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
 // more than 16 waves' keys is taken in parts, read again in every pass.  One workgroup, because its passes depend on each other; bound by
 // what one CU reads and by some 20 instructions and an LDS atomic per row: 32K rows 16 us, 4.5K rows 5.5 us (keys in LDS instead: 18; an
 // atomic behind a branch per row and pass: 22; keys read again in every pass, as a longer cache does: 43).
-template <int KPT>
-__global__ __launch_bounds__(EVICT_THREADS) void k_evict_select(Dims D, EvictArgs E, int32_t* __restrict__ keep) {
+// put(i, r): row r of the old cache becomes row i of the new one.
+template <int KPT, class Put>
+__device__ __forceinline__ void select_rows(const Dims& D, const EvictArgs& E, int unit, int len, Put put) {
     constexpr int WAVES = EVICT_THREADS / 64, PART = EVICT_THREADS * KPT, GROUPS = KPT / 4, COPIES = 2, PITCH = EVICT_BINS + 4;
     __shared__ __attribute__((aligned(16))) int hist[COPIES * PITCH + 64];
     __shared__ int sm[WAVES];
     __shared__ int2 s_count[WAVES];
     __shared__ uint32_t s_prefix;
     __shared__ int s_need, s_all;
-    const int unit = blockIdx.x, b = unit / D.Hkv, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int len = evict_len(E, b);
-    if (E.lens_o && unit % D.Hkv == 0 && tid == 0) E.lens_o[b] = min(len, E.budget);
-    keep += int64_t(unit) * E.budget;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (len <= E.budget) {
-        for (int r = tid; r < len; r += EVICT_THREADS) keep[r] = r;
+        for (int r = tid; r < len; r += EVICT_THREADS) put(r, r);
         return;
     }
     struct __attribute__((packed, aligned(4))) Four { uint32_t v[4]; };
@@ -217,7 +216,7 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_evict_select(Dims D, EvictArg
             if (need == 0) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (k[i] > prefix) keep[my_a++] = r0 + 256 * g + i;
+                    if (k[i] > prefix) put(my_a++, r0 + 256 * g + i);
                 return;
             }
 #pragma unroll
@@ -229,12 +228,19 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_evict_select(Dims D, EvictArg
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool ia = k[i] > prefix, ie = k[i] == prefix;
-                if (ia || (ie && my_e < need)) keep[my_a + min(my_e, need)] = r0 + 256 * g + i;
+                if (ia || (ie && my_e < need)) put(my_a + min(my_e, need), r0 + 256 * g + i);
                 my_a += ia ? 1 : 0;
                 my_e += ie ? 1 : 0;
             }
         });
     }
+}
+template <int KPT>
+__global__ __launch_bounds__(EVICT_THREADS) void k_evict_select(Dims D, EvictArgs E, int32_t* __restrict__ keep) {
+    const int unit = blockIdx.x, b = unit / D.Hkv, len = evict_len(E, b);
+    if (E.lens_o && unit % D.Hkv == 0 && threadIdx.x == 0) E.lens_o[b] = min(len, E.budget);
+    keep += int64_t(unit) * E.budget;
+    select_rows<KPT>(D, E, unit, len, [&](int i, int r) { keep[i] = r; });
 }
 
 // positions and weights of the rows that stay; weights behind them are zero, for the rows that come next
@@ -272,28 +278,21 @@ __global__ __launch_bounds__(256) void k_evict_rows(Dims D, EvictArgs E, const T
 // 8192 rows, 55 us = 4.9 TB/s (a block per workgroup: 119; through the caches the rows' next reader waits for the writes: 55 us here, but 87
 // instead of 77 us there).
 constexpr int EVICT_WG_ROWS = 256;
-template <int DH, int FMT>
-__global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantDims Q, const int32_t* __restrict__ keep, QuantDims N) {
-    constexpr int LPR = DH / 16, RPP = 256 / LPR, PASSES = EVICT_WG_ROWS / RPP, WROWS = 64 / LPR;      // rows of a wave and pass: 8 or 16
-    __shared__ float s_top[EVICT_WG_ROWS / WROWS], s_scale[EVICT_WG_ROWS / 16];
-    const int z = blockIdx.y, unit = blockIdx.z, b = unit / D.Hkv, h = unit % D.Hkv;
-    const int len = evict_len(E, b);
-    keep += int64_t(unit) * E.budget;
-    if (z == 2) {
-        evict_lists(E, unit, len, keep, blockIdx.x, gridDim.x);
-        return;
-    }
-    const int64_t row0 = int64_t(blockIdx.x) * EVICT_WG_ROWS;
-    const int rows = int(min(int64_t(EVICT_WG_ROWS), min(len, E.budget) - row0));
-    if (rows <= 0) return;
-    const int tid = threadIdx.x, sub = tid % LPR, rg = tid / LPR;
+struct QuantMoveLds { float top[EVICT_WG_ROWS / 8], scale[EVICT_WG_ROWS / 16]; };
+// By NT threads, `tid` of them: rows row0 .. of the new cache, `rows` of them, ROWS at most (none where not positive); from_row(i): the old
+// cache's row for i of these.  All threads of the workgroup call.
+template <int DH, int FMT, int NT, int ROWS, class Row>
+__device__ __forceinline__ void move_quant_rows(const QuantDims& Q, const QuantDims& N, int z, int unit, int b, int h, int64_t row0, int rows, int tid,
+                                                QuantMoveLds& sh, Row from_row) {
+    constexpr int LPR = DH / 16, RPP = NT / LPR, PASSES = ROWS / RPP, WROWS = 64 / LPR;      // rows of a wave and pass: 8 or 16
+    const int sub = tid % LPR, rg = tid / LPR;
     const uint8_t* src = (z ? Q.V : Q.K) + b * Q.st[0] + h * Q.st[1] + sub * 16;
     const float* scales = (z ? Q.Vs : Q.Ks) + int64_t(unit) * Q.nb;
     int from[PASSES];
     uint4 codes[PASSES];
     float scale[PASSES];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) from[p] = keep[row0 + min(p * RPP + rg, rows - 1)];      // rows past the end repeat the last one
+    for (int p = 0; p < PASSES; ++p) from[p] = rows > 0 ? from_row(min(p * RPP + rg, rows - 1)) : 0;      // rows past the end repeat the last one
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         codes[p] = stream_load(src + from[p] * Q.st[2]);
@@ -306,16 +305,16 @@ __global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantD
         code_values<FMT>(uint2{as_loaded(codes[p].z), as_loaded(codes[p].w)}, hi);
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(lo[i]), fabsf(hi[i])));
-        top = wave_max(p * RPP + rg < rows ? top * scale[p] : 0.0f);
-        if ((tid & 63) == 0) s_top[p * 4 + (tid >> 6)] = top;          // rows WROWS * (4 p + wave) ..
+        top = wave_max(top * scale[p]);                                // a row past the end repeats the last one: its block's maximum is the same
+        if ((tid & 63) == 0) sh.top[p * (NT / 64) + (tid >> 6)] = top;         // rows WROWS * (NT / 64 * p + wave) ..
     }
     __syncthreads();
     const int per = N.block / WROWS;                                   // such groups of rows in a block
     if (tid * N.block < rows) {
         float top = 0.0f;
-        for (int i = 0; i < per; ++i) top = fmaxf(top, s_top[tid * per + i]);
+        for (int i = 0; i < per; ++i) top = fmaxf(top, sh.top[tid * per + i]);
         const float s = quant_scale<FMT>(top);
-        s_scale[tid] = s;
+        sh.scale[tid] = s;
         (z ? N.Vs : N.Ks)[int64_t(unit) * N.nb + (row0 >> N.log_block) + tid] = s;
     }
     __syncthreads();
@@ -324,7 +323,7 @@ __global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantD
     for (int p = 0; p < PASSES; ++p) {
         const int r = p * RPP + rg;
         if (r >= rows) continue;
-        const float ratio = scale[p] * (1.0f / s_scale[r >> N.log_block]);      // exact for powers of two
+        const float ratio = scale[p] * (1.0f / sh.scale[r >> N.log_block]);      // exact for powers of two
         uint4 c = codes[p];
         if (ratio != 1.0f) {
             float lo[8], hi[8];
@@ -335,6 +334,73 @@ __global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantD
         }
         stream_store(dst + r * N.st[2], c);
     }
+}
+template <int DH, int FMT>
+__global__ __launch_bounds__(256) void k_evict_quant(Dims D, EvictArgs E, QuantDims Q, const int32_t* __restrict__ keep, QuantDims N) {
+    __shared__ QuantMoveLds sh;
+    const int z = blockIdx.y, unit = blockIdx.z, b = unit / D.Hkv, h = unit % D.Hkv;
+    const int len = evict_len(E, b);
+    keep += int64_t(unit) * E.budget;
+    if (z == 2) {
+        evict_lists(E, unit, len, keep, blockIdx.x, gridDim.x);
+        return;
+    }
+    const int64_t row0 = int64_t(blockIdx.x) * EVICT_WG_ROWS;
+    const int rows = int(min(int64_t(EVICT_WG_ROWS), min(len, E.budget) - row0));
+    if (rows <= 0) return;
+    move_quant_rows<DH, FMT, 256, EVICT_WG_ROWS>(Q, N, z, unit, b, h, row0, rows, threadIdx.x, sh, [&](int i) { return keep[row0 + i]; });
+}
+
+// Short caches (EVICT_SHORT rows at most): every workgroup selects the rows of its unit for itself, keeps those that become rows row0 .. of
+// the new cache in LDS, and moves them: one launch instead of two, which bound such calls, and no list in memory.  A workgroup takes as
+// many rows as give each CU one (SHORT_PIECES pieces of 16 bytes of K at most), in 8 bits the largest block.
+constexpr int EVICT_KPT = 8, EVICT_SHORT = EVICT_THREADS * EVICT_KPT, SHORT_CHUNK = 512, SHORT_PIECES = 8192, SHORT_QUANT_CHUNK = QUANT_MAX_BLOCK;
+__device__ __forceinline__ int select_chunk(const Dims& D, const EvictArgs& E, int unit, int len, int row0, int chunk, int32_t* list) {
+    if (E.lens_o && unit % D.Hkv == 0 && row0 == 0 && threadIdx.x == 0) E.lens_o[unit / D.Hkv] = min(len, E.budget);
+    select_rows<EVICT_KPT>(D, E, unit, len, [&](int i, int r) {
+        if (uint32_t(i - row0) < uint32_t(chunk)) list[i - row0] = r;
+    });
+    __syncthreads();
+    const int rows = max(0, min(chunk, min(len, E.budget) - row0));
+    const int64_t at = int64_t(unit) * E.cap;
+    for (int i = threadIdx.x; i < rows; i += EVICT_THREADS) {
+        E.acc_o[at + row0 + i] = E.acc[at + list[i]];
+        if (E.pos) E.pos_o[at + row0 + i] = E.pos[at + list[i]];
+    }
+    for (int64_t i = min(len, E.budget) + int64_t(blockIdx.x) * EVICT_THREADS + threadIdx.x; i < E.cap; i += int64_t(gridDim.x) * EVICT_THREADS)
+        E.acc_o[at + i] = 0.0f;
+    return rows;
+}
+// strides and rows in 16-byte pieces
+__global__ __launch_bounds__(EVICT_THREADS) void k_evict_short(Dims D, EvictArgs E, const uint4* __restrict__ K, const uint4* __restrict__ V, int pieces,
+                                                               int chunk, uint4* __restrict__ Ko, uint4* __restrict__ Vo) {
+    __shared__ int32_t list[SHORT_CHUNK];
+    const int unit = blockIdx.y, b = unit / D.Hkv, h = unit % D.Hkv, row0 = blockIdx.x * chunk;
+    const int rows = select_chunk(D, E, unit, evict_len(E, b), row0, chunk, list);
+    const int64_t at = b * D.ks[0] + h * D.ks[1];
+    const int sub = threadIdx.x % pieces, step = EVICT_THREADS / pieces;
+    for (int i = threadIdx.x / pieces; i < rows; i += 2 * step) {
+        const int j = min(i + step, rows - 1);               // the last row twice rather than loads in a branch
+        const int64_t a = at + list[i] * D.ks[2] + sub, c = at + list[j] * D.ks[2] + sub;
+        const uint4 k0 = stream_load(K + a), v0 = stream_load(V + a), k1 = stream_load(K + c), v1 = stream_load(V + c);
+        uint4 *Kn = Ko + at + row0 * D.ks[2] + sub, *Vn = Vo + at + row0 * D.ks[2] + sub;
+        stream_store(Kn + i * D.ks[2], k0);
+        stream_store(Vn + i * D.ks[2], v0);
+        if (i + step < rows) {
+            stream_store(Kn + j * D.ks[2], k1);
+            stream_store(Vn + j * D.ks[2], v1);
+        }
+    }
+}
+template <int DH, int FMT>
+__global__ __launch_bounds__(EVICT_THREADS) void k_evict_quant_short(Dims D, EvictArgs E, QuantDims Q, QuantDims N) {
+    __shared__ int32_t list[SHORT_QUANT_CHUNK];
+    __shared__ QuantMoveLds sh[2];
+    const int unit = blockIdx.y, b = unit / D.Hkv, h = unit % D.Hkv, row0 = blockIdx.x * SHORT_QUANT_CHUNK;
+    const int rows = select_chunk(D, E, unit, evict_len(E, b), row0, SHORT_QUANT_CHUNK, list);
+    const int z = __builtin_amdgcn_readfirstlane(threadIdx.x / (EVICT_THREADS / 2));
+    move_quant_rows<DH, FMT, EVICT_THREADS / 2, SHORT_QUANT_CHUNK>(Q, N, z, unit, b, h, row0, rows, threadIdx.x % (EVICT_THREADS / 2), sh[z],
+                                                                   [&](int i) { return list[i]; });
 }
 
 size_t cache_evict_ws_bytes(const Dims& D, int budget) { return align256(size_t(D.B) * D.Hkv * budget * 4); }
@@ -356,6 +422,14 @@ static EvictArgs evict_args(const Dims& D, const int32_t* lens, int len, int bud
     return E;
 }
 
+// One launch where a workgroup has all keys of its unit in registers and every workgroup a CU of its own, so that the selections that are
+// made several times cost no time.  bf16, d 128, one launch and two: 8 heads, 4501 rows of which 2048 stay 12.4 and 15.5 us, 32 heads (256
+// workgroups) 21.0 and 22.3, 32 heads of which 6000 stay (384) 53 and 43; 8 bits, 4 heads, 8111 rows of
+// which 2048 stay, and reading them back, 16.4 and 18.7.
+static bool short_eviction(const Dims& D, int len, int rows, int chunk) {
+    return len <= EVICT_SHORT && (int64_t(rows) + chunk - 1) / chunk * D.B * D.Hkv <= 256;
+}
+
 static void launch_select(const Dims& D, const EvictArgs& E, int32_t* keep, hipStream_t st) {
     const int per = (E.len + EVICT_THREADS - 1) / EVICT_THREADS;      // keys per thread
     LRSA_TIMED_LAUNCH("k_evict_select", st, (per <= 4 ? k_evict_select<4> : per <= 8 ? k_evict_select<8> : per <= 16 ? k_evict_select<16> :
@@ -365,6 +439,16 @@ static void launch_select(const Dims& D, const EvictArgs& E, int32_t* keep, hipS
 template <typename T>
 static hipError_t run_evict(const Dims& D, const EvictArgs& E, const void* K, const void* V, void* Ko, void* Vo, int32_t* keep, hipStream_t st) {
     const int rows = E.len < E.budget ? E.len : E.budget;
+    const int pieces = D.d / Elem<T>::VEC, step = EVICT_THREADS / pieces;      // 16-byte pieces of a row; rows that move at once
+    const int64_t share = (int64_t(rows) * D.B * D.Hkv + 255) / 256, up = (share + step - 1) / step * step;
+    const int most = SHORT_PIECES / pieces < SHORT_CHUNK ? SHORT_PIECES / pieces : SHORT_CHUNK, chunk = up < step ? step : up < most ? int(up) : most;
+    if (short_eviction(D, E.len, rows, chunk)) {
+        Dims P = D;
+        for (int i = 0; i < 3; ++i) P.ks[i] = D.ks[i] / Elem<T>::VEC;
+        LRSA_TIMED_LAUNCH("k_evict_short", st, k_evict_short, dim3(rows ? (rows + chunk - 1) / chunk : 1, D.B * D.Hkv), dim3(EVICT_THREADS), 0, st, P, E,
+                          (const uint4*)K, (const uint4*)V, pieces, chunk, (uint4*)Ko, (uint4*)Vo);
+        return hipGetLastError();
+    }
     launch_select(D, E, keep, st);
     const unsigned blocks = unsigned((int64_t(rows) * (D.d / Elem<T>::VEC) + 255) / 256);
     LRSA_TIMED_LAUNCH("k_evict_rows", st, k_evict_rows<T>, dim3(blocks ? blocks : 1, 3, D.B * D.Hkv), dim3(256), 0, st, D, E, (const T*)K, (const T*)V,
@@ -381,6 +465,18 @@ hipError_t launch_cache_evict_quant(const Dims& D, const QuantDims& Q, const Qua
     const EvictArgs E = evict_args(D, lens, max_len, budget, recent, pos, acc, pos_o, acc_o, lens_o);
     int32_t* keep = (int32_t*)ws;
     const int rows = max_len < budget ? max_len : budget;
+    if (short_eviction(D, max_len, rows, SHORT_QUANT_CHUNK)) {
+        const dim3 grid(rows ? (rows + SHORT_QUANT_CHUNK - 1) / SHORT_QUANT_CHUNK : 1, D.B * D.Hkv);
+#define LRSA_EVICT_SHORT(DH_, FMT_) \
+    LRSA_TIMED_LAUNCH("k_evict_quant_short", st, (k_evict_quant_short<DH_, FMT_>), grid, dim3(EVICT_THREADS), 0, st, D, E, Q, N)
+        if (Q.fmt == QUANT_INT8) {
+            if (D.d == 64) LRSA_EVICT_SHORT(64, QUANT_INT8); else LRSA_EVICT_SHORT(128, QUANT_INT8);
+        } else {
+            if (D.d == 64) LRSA_EVICT_SHORT(64, QUANT_E4M3); else LRSA_EVICT_SHORT(128, QUANT_E4M3);
+        }
+#undef LRSA_EVICT_SHORT
+        return hipGetLastError();
+    }
     launch_select(D, E, keep, st);
     const dim3 grid(unsigned(rows ? (rows + EVICT_WG_ROWS - 1) / EVICT_WG_ROWS : 1), 3, D.B * D.Hkv);
 #define LRSA_EVICT_QUANT(DH_, FMT_) LRSA_TIMED_LAUNCH("k_evict_quant", st, (k_evict_quant<DH_, FMT_>), grid, dim3(256), 0, st, D, E, Q, keep, N)

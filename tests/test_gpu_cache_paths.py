@@ -1,5 +1,5 @@
-"""Attention over the inference-time caches where its work is divided in other ways: short caches in one launch and their limits, long
-walks of many columns, more sequences than a wave has lanes, rows far apart.  Oracle and tolerances as in test_gpu_cache_weights.py.
+"""Attention over the inference-time caches and eviction where their work is divided in other ways: short caches in one launch and their
+limits, long walks of many columns, more sequences than a wave has lanes, many heads, rows far apart.  Oracle and tolerances as in test_gpu_cache_weights.py.
 """
 import numpy as np
 import pytest
@@ -7,7 +7,7 @@ import torch
 
 import paper_2506_11498_amd as lrsa
 from oracle import lrsa_cache_ops as ops
-from test_gpu_cache_quant import CODES, check_attention, i32, make_cache
+from test_gpu_cache_quant import CODES, check_attention, host, i32, make_cache
 from test_gpu_cache_weights import DEV, DT, close_attention, params
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +109,52 @@ def test_rows_far_apart(dtype):
         lrsa.lrsa_cache_evict(p, K, V, None, acc, n, 50, 10, Ko, Vo, None, acc_o)
         got.append((O, lse, O1, lse1, acc, Ko[:, :, :50].clone(), Vo[:, :, :50].clone(), acc_o))
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype,d,B,Hkv,length,budget", [("bf16", 64, 40, 8, 300, 120), ("f32", 64, 64, 1, 5000, 2100), ("bf16", 128, 16, 8, 1000, 999), ("f32", 128, 3, 1, 8192, 8191),
+                                                         ("bf16", 128, 1, 2, 8193, 100), ("bf16", 64, 300, 1, 0, 5), ("f32", 128, 2, 2, 200, 100)])
+def test_evictions_of_many_heads_and_at_the_limits(dtype, d, B, Hkv, length, budget):
+    """One launch and two: on both sides of the length and of the number of workgroups; positions, weights and rows of all heads."""
+    cap = max(length, budget) + 3
+    g = torch.Generator(device=DEV).manual_seed(length + B)
+    K, V = (torch.randn((B, cap, Hkv, d), generator=g, device=DEV).to(DT[dtype]).permute(0, 2, 1, 3) for _ in range(2))
+    acc = torch.randint(0, 50, (B, Hkv, cap), generator=g, device=DEV).float()
+    pos = torch.arange(cap, dtype=torch.int32, device=DEV).expand(B, Hkv, cap).contiguous()
+    p = params(B, Hkv, Hkv, cap, d, K.stride(), DT[dtype], sink=2)
+    Ko, Vo, po, ao = torch.full_like(K, 3), torch.full_like(V, 3), torch.full_like(pos, -5), torch.full_like(acc, -5)
+    new = lrsa.lrsa_cache_evict(p, K, V, pos, acc, length, budget, 3, Ko, Vo, po, ao)
+    assert new == min(length, budget)
+    want = torch.tensor(np.stack([ops.evict_rows(a, length, 2, 3, budget) for a in acc.reshape(-1, cap).cpu().numpy()]), device=DEV).reshape(B, Hkv, new).long()
+    assert torch.equal(po[:, :, :new].long(), want) and torch.equal(ao[:, :, :new], acc.gather(2, want))
+    at = want[..., None].expand(B, Hkv, new, d)
+    assert torch.equal(Ko[:, :, :new], K.gather(2, at)) and torch.equal(Vo[:, :, :new], V.gather(2, at))
+    for t, fill in ((Ko, 3), (Vo, 3), (po, -5), (ao, 0)):
+        assert bool((t[:, :, new:] == fill).all())
+
+
+@pytest.mark.parametrize("fmt,d,B,Hkv,block,n,budget", [("int8", 128, 40, 8, 64, 300, 130), ("e4m3", 64, 64, 1, 128, 5000, 700), ("int8", 64, 16, 8, 16, 1000, 256), ("e4m3", 128, 3, 1, 128, 8192, 8100),
+                                                        ("int8", 128, 2, 1, 32, 8193, 100), ("e4m3", 64, 130, 2, 16, 90, 50)])
+def test_evictions_of_many_heads_in_eight_bits(fmt, d, B, Hkv, block, n, budget):
+    """The same of ragged sequences.  Every second one is compared."""
+    cap = n + 3
+    lens = [n - (29 * b) % n for b in range(B)]
+    lens[-1] = 0
+    g = torch.Generator().manual_seed(B + n)
+    cache, raw, scales = make_cache(B, Hkv, cap, d, fmt, block, g, lens, strided=False)
+    out, _, _ = make_cache(B, Hkv, cap, d, fmt, block, g)
+    acc = torch.randint(0, 1 << 20, (B, Hkv, cap), generator=g).float()
+    p = params(B, Hkv, Hkv, cap, d, (Hkv * cap * d, cap * d, d, 1), torch.bfloat16, sink=2)
+    ao, lo = torch.full((B, Hkv, cap), -3.0, device=DEV), i32([-3] * B)
+    lrsa.lrsa_cache_evict_quant(p, cache, None, acc.to(DEV), i32(lens), n, budget, 3, out, None, ao, lo)
+    assert lo.cpu().tolist() == [min(x, budget) for x in lens]
+    got = host(out)
+    for b in range(0, B, 2):
+        new = min(lens[b], budget)
+        for h in range(Hkv):
+            rows = ops.evict_rows(acc[b, h].double().numpy(), lens[b], 2, 3, budget)
+            assert torch.equal(ao[b, h, :new].cpu(), acc[b, h][torch.from_numpy(rows)]) and bool((ao[b, h, new:] == 0).all())
+            for z in range(2):
+                x = ops.values(raw[z][b, h].numpy()[:lens[b]], scales[z][b, h].numpy(), block, fmt)[rows] if lens[b] else np.zeros((0, d))
+                codes, s = ops.evict_blocks(x, block, fmt)
+                assert np.array_equal(ops.decode(got[z][b, h, :new], fmt), ops.decode(codes, fmt))
+                assert np.array_equal(got[2 + z][b, h, :len(s)].astype(np.float64), s)
