@@ -649,7 +649,12 @@ static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
     // Two workgroups share a CU (registers), so 512 run at once.  With more units than half of that some would have two slices and some
     // one: then several rounds, of few more slices than units.  8 KV heads, 64 requests of 2048 rows: units + 256 55 us, + 512 58,
     // + 768 67, + 2048 71; 33 of 4096: 80, 70, 65, 70.
-    const int64_t most = units <= 256 ? 512 : units + 512;
+    // With few units of long bf16 rows, one workgroup per CU keeps enough loads in flight, and half as many slices are joined: 8 KV heads, bf16,
+    // d 128, 4 columns, 256 and 512 workgroups: 1 request of 16K rows 16.1 us and 18.7, of 128K 50.7 and 54.0, 4 of 20K 35.0 and 38.5, of 11K
+    // to 32K each 30.2 and 31.0, but 8 of those 76.5 and 75.1; 20 columns: 1 of 20K 21.6 and 23.7, 4 of 40K 90 and 84; d 64, 4 of
+    // 40K 39.9 and 37.2; fp32 71 and 64.5.
+    const bool few = D.dtype == 1 && D.d == 128 && units <= (D.G * tokens <= 16 ? 32 : 8);
+    const int64_t most = few ? 256 : units <= 256 ? 512 : units + 512;
     const int64_t tiles = (int64_t(max_len) + QT - 1) / QT, fine = units * ((tiles + DEC_WAVES - 1) / DEC_WAVES);
     const float up = 1.0f + 0x1p-20f;
     P.s.most = int(most);
