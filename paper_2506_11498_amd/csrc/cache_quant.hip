@@ -145,7 +145,9 @@ __device__ __forceinline__ int slice_tiles(const Dims& D, const SeqLens& L, cons
 // the logit, that of V the weight, in fp32 (4 such rows share a block: blocks are multiples of 16).  Queries of fp32 enter as
 // three bf16 terms, which hold all 24 bits, and so do the weights.
 // A wave takes 16 * NG columns.  If these are all, the 4 waves take the tiles in turn (SOLE): every code is read by one wave of the
-// chip, past the caches.  Where there are more, `groups` (2 or 4) waves take the same tile, so that its codes come from memory once, and
+// chip, and past the caches (PAST) where the cache is as large as the Infinity Cache (256 MB), which would keep little of it until the next call.  8 KV
+// heads of 4 query heads, us per call on the same cache, through and past the caches: 40 MB 14.6 and 16.2, 159 MB 32.5 and 35.3, 269 MB
+// 47.6 and 51.9, 537 MB 102 and 95; on others in turn: 16.2 and 16.8, 37.8 and 36.5, 54.5 and 52.3, 102 and 95.  Where there are more, `groups` (2 or 4) waves take the same tile, so that its codes come from memory once, and
 // beyond 4 times as many columns the slice is walked again.  NG = 2 halves the unpacking of codes, which bounds many columns (8 requests of
 // 32K rows, 20 columns: 107 us, with NG = 1 128; 64 columns: 171 and 212); it needs registers that fp32 queries of 128 channels do not
 // leave, and long walks.
@@ -165,9 +167,9 @@ struct QuantRows {                           // of one unit
     int64_t st;
     int log_block;
 };
-template <bool SOLE, typename V>
+template <bool PAST, typename V>
 __device__ __forceinline__ V load_codes(const uint8_t* p) {
-    if constexpr (SOLE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
     return *reinterpret_cast<const V*>(p);
 }
 
@@ -198,7 +200,7 @@ __device__ __forceinline__ void codes_bf16_columns(uint32_t w0, uint32_t w1, uin
 }
 
 // r: the tile's first row (wave-uniform), of rows up to `last`: rows past the end repeat it, their weight will be 0
-template <int DH, bool SOLE>
+template <int DH, bool PAST>
 __device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantRows& R, int r, int q4, int c, int last) {
     const uint8_t *K = R.K + r * R.st, *V = R.V + r * R.st;
     const uint32_t most = min(last - r, QT - 1), st = uint32_t(R.st);        // rows are less than 2^24 bytes apart
@@ -207,10 +209,10 @@ __device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantRow
     for (int kb = 0; kb < 2; ++kb) {
         const uint32_t row = off(16 * kb + c) + q4 * 16;
 #pragma unroll
-        for (int i = 0; i < DH / 64; ++i) t.k[kb][i] = load_codes<SOLE, u32x4>(K + row + i * 64);
+        for (int i = 0; i < DH / 64; ++i) t.k[kb][i] = load_codes<PAST, u32x4>(K + row + i * 64);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t.v[j] = load_codes<SOLE, typename QPiece<DH>::type>(V + (off(4 * q4 + j % 4 + j / 4 * 16) + c * (DH / 16)));
+    for (int j = 0; j < 8; ++j) t.v[j] = load_codes<PAST, typename QPiece<DH>::type>(V + (off(4 * q4 + j % 4 + j / 4 * 16) + c * (DH / 16)));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t block = (r + min(uint32_t(16 * i + 4 * q4), most)) >> R.log_block;
@@ -314,7 +316,7 @@ __device__ __forceinline__ void query_terms(const float* q, bf16x8 (&f)[3]) {
 template <typename T> constexpr int Q_TERMS = sizeof(T) == 2 ? 1 : 3;
 template <typename T, int DH> constexpr int MOST_GROUPS = sizeof(T) == 2 || DH == 64 ? 2 : 1;      // NG
 
-template <typename T, int DH, int FMT, int NG, bool SOLE, bool ACC>
+template <typename T, int DH, int FMT, int NG, bool SOLE, bool PAST, bool ACC>
 __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDims Q, const T* __restrict__ q, int tokens, const int32_t* __restrict__ lens,
                                                                  int max_len, QuantSlices S, QuantSeq* __restrict__ seqs, float* __restrict__ part,
                                                                  float* __restrict__ logits, int64_t lrows, int pitch) {
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
         int r = r0 + wave / groups * QT;
         if (gn > 0 && r < r1) {
             const int end = r + (r1 - 1 - r) / step * step;      // the wave's last tile
-            auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, SOLE>(t, R, min(row, end), q4, c, r1 - 1); };
+            auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, PAST>(t, R, min(row, end), q4, c, r1 - 1); };
             QuantTile<DH> A, B;
             load(A, r);
             bf16x8 qf[NG][TERMS][DH / 32];
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(64 * SHORT_WAVES) void k_decode_quant_short(Dims D,
     if (r < len) {
         constexpr int STEP = SHORT_WAVES * QT;
         const int end = r + (len - 1 - r) / STEP * STEP, col = min(c, cols - 1);
-        auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, true>(t, R, min(row, end), q4, c, len - 1); };
+        auto load = [&](QuantTile<DH>& t, int row) { load_quant_tile<DH, false>(t, R, min(row, end), q4, c, len - 1); };
         QuantTile<DH> A0, B0;
         load(A0, r);
         bf16x8 qf[1][TERMS][DH / 32];
@@ -634,6 +636,7 @@ hipError_t launch_read_quant(const Dims& D, const QuantDims& Q, const int32_t* l
 // 8K 60.6 and 56.7, 16K (62) 98.4 and 87.5; 8 tokens: 26.2 and 31.4, 38.8 and 41.8, 61.9 and 58.0; d 64: 18.9 and 21.4, 26.1 and 28.4,
 // 39.7 and 39.5.
 constexpr int WIDE_TILES = 40;
+constexpr int64_t PAST_BYTES = int64_t(256) << 20;      // see k_decode_quant
 namespace {
 struct QuantPlan { QuantSlices s; int grid, pitch; bool wide; int64_t rows; size_t part, logits, bytes; };
 }
@@ -713,16 +716,18 @@ static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void
 #undef LRSA_DECODE_SHORT
         return hipGetLastError();
     }
-#define LRSA_DECODE_QUANT(DH_, FMT_, NG_, SOLE_)                                                                                          \
+    const bool past = int64_t(D.B) * D.Hkv * max_len * D.d * 2 >= PAST_BYTES;
+#define LRSA_DECODE_QUANT(DH_, FMT_, NG_, SOLE_, PAST_)                                                                                   \
     LRSA_TIMED_LAUNCH("k_decode_quant", st,                                                                                               \
-                      (acc_out ? k_decode_quant<T, DH_, FMT_, NG_, SOLE_, true> : k_decode_quant<T, DH_, FMT_, NG_, SOLE_, false>),        \
+                      (acc_out ? k_decode_quant<T, DH_, FMT_, NG_, SOLE_, PAST_, true> : k_decode_quant<T, DH_, FMT_, NG_, SOLE_, PAST_, false>), \
                       dim3(P.grid), dim3(DEC_THREADS), 0, st, D, Q, (const T*)q, tokens, lens, max_len, P.s, seqs, part, logits, P.rows,   \
                       P.pitch)
 #define LRSA_DECODE_QUANT_FMT(DH_, FMT_)                                                            \
-    if (A.cols <= 16) LRSA_DECODE_QUANT(DH_, FMT_, 1, true);                                        \
-    else if (!P.wide) LRSA_DECODE_QUANT(DH_, FMT_, 1, false);                                       \
-    else if (A.cols <= 16 * MOST) LRSA_DECODE_QUANT(DH_, FMT_, MOST, true);                         \
-    else LRSA_DECODE_QUANT(DH_, FMT_, MOST, false)
+    if (A.cols <= 16 && past) LRSA_DECODE_QUANT(DH_, FMT_, 1, true, true);                          \
+    else if (A.cols <= 16) LRSA_DECODE_QUANT(DH_, FMT_, 1, true, false);                            \
+    else if (!P.wide) LRSA_DECODE_QUANT(DH_, FMT_, 1, false, false);                                \
+    else if (A.cols <= 16 * MOST) LRSA_DECODE_QUANT(DH_, FMT_, MOST, true, true);                   \
+    else LRSA_DECODE_QUANT(DH_, FMT_, MOST, false, false)
 #define LRSA_DECODE_QUANT_DH(FMT_)                                                                  \
     if (D.d == 64) {                                                                                \
         constexpr int MOST = MOST_GROUPS<T, 64>;                                                    \

@@ -327,9 +327,20 @@ hipError_t launch_cache_compress_ws(const Dims& D, void* Kc, void* Vc, int32_t* 
 // merge, 5.4 TB/s), by latency for a short one (2.3K rows, 2 KV heads: 24.2 -> 10.7 us).  In the vector pipe, one lane's
 // dot products and a shuffle through LDS per row and head bounded it.  Errors against 64 bits as before: O differs from
 // the rounded exact value in at most 0.2 % of the elements.
-// FAST: rows are less than 2^24 bytes apart, so that a lane's place in a tile is a 32-bit offset from a wave-uniform address, and the heads
-// of a group fit one pass, so that every row is read once, past the caches.  The same values either way (8 requests of 16.4K rows,
-// 8 KV heads, 4 query heads each: 103.5 and 97 us, with the logits written 117 and 111).
+// How rows are read (the same values in all):
+//   ANY     64-bit addresses
+//   NEAR    rows are less than 2^24 bytes apart, so that a lane's place in a tile is a 32-bit offset from a wave-uniform address
+//   PAST    the same past the caches, where the heads of a group fit one pass, so that every row is read once, and the cache is larger than
+//           PAST_BYTES: the Infinity Cache (256 MB) would keep little of it until the next call.  8 KV heads of 4 query heads, us per
+//           call on the same cache, NEAR and PAST: 40 MB 15 and 16, 159 MB 29 and 33, 319 MB 53 and 57, 398 MB 73 and 70, 537 MB 96
+//           and 90, 786 MB 137 and 127; on others in turn: 16.7 and 18.2, 34 and 35, 60 and 58, 73 and 71, 96 and 91.
+enum { ROWS_ANY, ROWS_NEAR, ROWS_PAST };
+constexpr int64_t PAST_BYTES = int64_t(320) << 20;
+template <int HOW, typename V>
+__device__ __forceinline__ V load_piece(const char* p) {
+    if constexpr (HOW == ROWS_PAST) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    return *reinterpret_cast<const V*>(p);
+}
 template <int DH> struct VPiece { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <> struct VPiece<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <int DH> struct DecTile {
@@ -338,22 +349,21 @@ template <int DH> struct DecTile {
 };
 // the tile from row r on, of rows up to `last`: rows past the end repeat it, weight 0.  kr, vr: the lane's first rows of K and V, kc, vc: its
 // channels
-template <int DH, bool FAST>
+template <int DH, int HOW>
 __device__ __forceinline__ void load_tile(DecTile<DH>& t, const bf16_t* K, const bf16_t* V, int64_t stride, int r, int kr, int vr, int kc, int vc,
                                           int last) {
     typedef typename VPiece<DH>::type piece;
-    if constexpr (FAST) {
+    if constexpr (HOW != ROWS_ANY) {
         const char *Kr = reinterpret_cast<const char*>(K + r * stride), *Vr = reinterpret_cast<const char*>(V + r * stride);
         const uint32_t most = min(last - r, DEC_TILE - 1), st = uint32_t(stride) * 2;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const uint32_t at = __umul24(min(uint32_t(kr + 4 * kb), most), st) + kc * 2;
 #pragma unroll
-            for (int kk = 0; kk < DH / 32; ++kk) t.k[kb][kk] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(Kr + at + kk * 64));
+            for (int kk = 0; kk < DH / 32; ++kk) t.k[kb][kk] = load_piece<HOW, bf16x8>(Kr + at + kk * 64);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            t.v[j] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(Vr + (__umul24(min(uint32_t(vr + j), most), st) + vc * 2)));
+        for (int j = 0; j < 8; ++j) t.v[j] = load_piece<HOW, piece>(Vr + (__umul24(min(uint32_t(vr + j), most), st) + vc * 2));
     } else {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -426,7 +436,7 @@ __device__ __forceinline__ void use_tile(DecState<DH>& st, const DecTile<DH>& t,
     }
 }
 
-template <int DH, bool LOGITS, bool FAST>
+template <int DH, bool LOGITS, int HOW>
 __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf16_t* __restrict__ q, const bf16_t* __restrict__ Kc,
                                                                 const bf16_t* __restrict__ Vc, int len, int per, int splits,
                                                                 float* __restrict__ part, float* __restrict__ logits, int64_t lrows, int pitch) {
@@ -462,7 +472,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_mfma(Dims D, const bf
         if (r < r1) {
             DecTile<DH> A, B;
             const int end = r + (r1 - 1 - r) / STEP * STEP;      // the wave's last tile
-            auto load = [&](DecTile<DH>& t, int row) { load_tile<DH, FAST>(t, Kh, Vh, D.ks[2], min(row, end), kr, vr, q4 * 8, c * CPL, r1 - 1); };
+            auto load = [&](DecTile<DH>& t, int row) { load_tile<DH, HOW>(t, Kh, Vh, D.ks[2], min(row, end), kr, vr, q4 * 8, c * CPL, r1 - 1); };
             load(A, r);
             for (;;) {
                 load(B, r + STEP);
@@ -700,10 +710,11 @@ static void decode_slices(const Dims& D, const void* q, const void* Kc, const vo
                           int64_t lrows, int pitch, hipStream_t st) {
     if (D.dtype == 1) {
         const int per = ((len + splits - 1) / splits + DEC_TILE - 1) / DEC_TILE * DEC_TILE;
-        const bool fast = D.G <= 16 && D.ks[2] < 1 << 23;
+        const bool near = D.ks[2] < 1 << 23, past = near && D.G <= 16 && int64_t(D.B) * D.Hkv * len * D.d * 4 > PAST_BYTES;
         LRSA_TIMED_LAUNCH("k_decode_mfma", st,
-                          (D.d == 64 ? (fast ? k_decode_mfma<64, LOGITS, true> : k_decode_mfma<64, LOGITS, false>)
-                                     : (fast ? k_decode_mfma<128, LOGITS, true> : k_decode_mfma<128, LOGITS, false>)), dim3(splits, D.B * D.Hkv),
+                          (D.d == 64 ? (past ? k_decode_mfma<64, LOGITS, ROWS_PAST> : near ? k_decode_mfma<64, LOGITS, ROWS_NEAR> : k_decode_mfma<64, LOGITS, ROWS_ANY>)
+                                     : (past ? k_decode_mfma<128, LOGITS, ROWS_PAST> : near ? k_decode_mfma<128, LOGITS, ROWS_NEAR> : k_decode_mfma<128, LOGITS, ROWS_ANY>)),
+                          dim3(splits, D.B * D.Hkv),
                           dim3(DEC_THREADS), 0, st, D, (const bf16_t*)q, (const bf16_t*)Kc, (const bf16_t*)Vc, len, per, splits, part, logits,
                           lrows, pitch);
     } else {

@@ -158,3 +158,54 @@ def test_evictions_of_many_heads_in_eight_bits(fmt, d, B, Hkv, block, n, budget)
                 codes, s = ops.evict_blocks(x, block, fmt)
                 assert np.array_equal(ops.decode(got[z][b, h, :new], fmt), ops.decode(codes, fmt))
                 assert np.array_equal(got[2 + z][b, h, :len(s)].astype(np.float64), s)
+
+
+@pytest.mark.parametrize("d,B,n", [(128, 9, 10300), (64, 17, 10301)])
+def test_large_bf16_caches(d, B, n):
+    """Caches of more than 320 MiB, read past the GPU's caches; two units are compared, and the bits with and without weights."""
+    Hkv, G, T, cap = 8, 5, torch.bfloat16, n + 3
+    g = torch.Generator(device=DEV).manual_seed(n)
+    K, V = (torch.randn((B, Hkv, cap, d), generator=g, device=DEV, dtype=torch.float32).to(T) for _ in range(2))
+    K[:, :, n:], V[:, :, n:] = float("nan"), float("inf")
+    q = torch.randn((B, Hkv * G, d), generator=g, device=DEV).to(T)
+    p = params(B, Hkv * G, Hkv, cap, d, K.stride(), T)
+    acc = torch.full((B, Hkv, cap), -7.0, device=DEV)
+    O, lse, _ = lrsa.lrsa_decode_attn_acc(p, q, K, V, n, None, acc)
+    O1, lse1 = lrsa.lrsa_decode_attn(p, q, K, V, n)
+    assert torch.equal(O, O1) and torch.equal(lse, lse1) and bool((acc[:, :, n:] == -7.0).all())
+    for b, h in ((0, 3), (B - 1, 7)):
+        hs = slice(h * G, (h + 1) * G)
+        Kh, Vh, qs = (x.double().cpu().numpy() for x in (K[b, h, :n], V[b, h, :n], q[b, hs][:, None]))
+        O_ref, lse_ref, w = ops.attend(qs, Kh, Vh)
+        eps = close_attention(O[b, hs][:, None].double().cpu().numpy(), lse[b, hs][:, None].double().cpu().numpy(), qs, Kh, Vh, O_ref, lse_ref, d ** -0.5, 2.0 ** -8)
+        assert np.all(np.abs(acc[b, h, :n].double().cpu().numpy() - w) <= 2 * eps * w + 1e-37)
+
+
+@pytest.mark.parametrize("fmt,dtype,d,B,n,T", [("int8", "bf16", 128, 8, 16500, 1), ("e4m3", "f32", 64, 17, 16400, 2)])
+def test_large_caches_in_eight_bits(fmt, dtype, d, B, n, T):
+    """The same of more than 256 MiB of codes, sequences of unequal length."""
+    Hkv, G, block, cap = 8, 4, 64, n + 5
+    lens = [n - 11 * b for b in range(B)]
+    lens[2] = 0
+    g = torch.Generator(device=DEV).manual_seed(n)
+    raw = [torch.randint(0, 256, (B, Hkv, cap, d), generator=g, device=DEV, dtype=torch.uint8) for _ in range(2)]
+    if fmt == "e4m3":
+        raw = [r.bitwise_and_(0xbf) for r in raw]
+        for r in raw:
+            r[(r & 0x7f) == 0x7f] = 0x31
+    scales = [torch.exp2(torch.randint(-9, -5, (B, Hkv, -(-cap // block)), generator=g, device=DEV).float()) * (64 if fmt == "e4m3" else 1) for _ in range(2)]
+    cache = lrsa.QuantCache(*(r.view(CODES[fmt]) for r in raw), *scales, block)
+    q = torch.randn((B, Hkv * G, T, d), generator=g, device=DEV).to(DT[dtype])
+    p = params(B, Hkv * G, Hkv, cap, d, (Hkv * cap * d, cap * d, d, 1), DT[dtype])
+    out = torch.full((B, Hkv, cap), -7.0, device=DEV)
+    O, lse = lrsa.lrsa_decode_attn_quant(p, q, cache, i32(lens), n, None, out)
+    O1, lse1 = lrsa.lrsa_decode_attn_quant(p, q, cache, i32(lens), n)
+    assert torch.equal(O, O1) and torch.equal(lse, lse1)
+    assert all(bool((out[b, :, m:] == -7.0).all()) for b, m in enumerate(lens)) and bool((O[2] == 0).all()) and bool(torch.isneginf(lse[2]).all())
+    for b, h in ((1, 0), (B - 1, 6)):
+        hs, m = slice(h * G, (h + 1) * G), lens[b]
+        K, V = (ops.values(r[b, h, :m].cpu().numpy(), s[b, h, :-(-m // block)].cpu().numpy(), block, fmt) for r, s in zip(raw, scales))
+        qs = q[b, hs].double().cpu().numpy()
+        O_ref, lse_ref, w = ops.attend(qs, K, V)
+        eps = close_attention(O[b, hs].double().cpu().numpy(), lse[b, hs].double().cpu().numpy(), qs, K, V, O_ref, lse_ref, d ** -0.5, 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
+        assert np.all(np.abs(out[b, h, :m].double().cpu().numpy() - w) <= 2 * eps * w + 1e-37)
