@@ -331,6 +331,7 @@ typedef struct {
 /* Rows lens[b] .. lens[b] + counts[b] - 1 of sequence b become the first counts[b] rows of K and V.  Where the first of them
  * falls into a block with older rows, that block's scale grows if it must and its older codes are rounded to the new scale.  Rows
  * that would lie at or behind cap are dropped; lens is not changed; codes behind the new rows are left as they were.
+ * Sequences and heads of a cache that is written must not share rows (no stride of 0), and its K and V are two.
  *   K, V   : [B, Hkv, tokens, d_h] by kv_stride, dtype `dtype`                     (device, read)
  *   counts : [B] int32, 0 <= counts[b] <= tokens (others count as the nearer bound), or NULL: tokens of every sequence */
 int lrsa_cache_append_quant(const lrsa_params *p, const lrsa_quant_cache *c, const void *K, const void *V, int32_t tokens,

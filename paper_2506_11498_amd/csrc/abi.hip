@@ -505,6 +505,17 @@ int make_quant(const char* who, const lrsa::Dims& D, const lrsa_quant_cache* c, 
     return LRSA_OK;
 }
 
+// rows that a call writes: no two in one place
+int check_written(const char* who, const lrsa::Dims& D, const int64_t (&st)[3]) {
+    if ((D.B > 1 && st[0] == 0) || (D.Hkv > 1 && st[1] == 0))
+        return fail(LRSA_ERR_INVALID_ARG, "%s: sequences or heads share their rows (stride 0), which would be written", who);
+    return LRSA_OK;
+}
+int check_written(const char* who, const lrsa::Dims& D, const lrsa::QuantDims& Q) {
+    if (Q.K == Q.V || Q.Ks == Q.Vs) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V of the cache that is written must be two", who);
+    return check_written(who, D, Q.st);
+}
+
 int check_evict(const char* who, const lrsa::Dims& D, int32_t len, int32_t budget, int32_t recent) {
     if (len < 0 || len > D.n) return fail(LRSA_ERR_INVALID_ARG, "%s: length %d outside [0, cap=%d]", who, len, D.n);
     if (recent < 0 || budget < 1 || budget > D.n || (int64_t)D.S + recent > budget)
@@ -560,7 +571,7 @@ int lrsa_cache_evict(const lrsa_params* p, const void* Kc, const void* Vc, const
     if (misaligned16(Kc) || misaligned16(Vc) || misaligned16(Ko) || misaligned16(Vo))
         return fail(LRSA_ERR_INVALID_ARG, "%s: Kc, Vc, Ko and Vo must be 16-byte aligned", who);
     if (Ko == Kc || Vo == Vc || Ko == Vc || Vo == Kc || Ko == Vo) return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must not be the old one", who);
-    if ((rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
+    if ((rc = check_written(who, D, D.ks)) != LRSA_OK || (rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
     if ((rc = check_ws_bytes(who, lrsa::cache_evict_ws_bytes(D, budget), ws, ws_bytes)) != LRSA_OK) return rc;
     rc = hip_result(lrsa::launch_cache_evict(D, Kc, Vc, pos, acc, len, budget, recent, Ko, Vo, pos_o, acc_o, ws, (hipStream_t)stream), who);
     if (rc == LRSA_OK) *len_out = len < budget ? len : budget;
@@ -577,6 +588,7 @@ int lrsa_cache_append_quant(const lrsa_params* p, const lrsa_quant_cache* c, con
     if (tokens < 1) return fail(LRSA_ERR_INVALID_ARG, "%s: tokens must be >= 1", who);
     if (!K || !V || !lens) return fail(LRSA_ERR_INVALID_ARG, "%s: K, V and lens must not be NULL", who);
     if (misaligned16(K) || misaligned16(V)) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
+    if ((rc = check_written(who, D, Q)) != LRSA_OK) return rc;
     if (!lrsa::grid_fits(Q.nb, 256)) return fail(LRSA_ERR_UNSUPPORTED, "%s: cap %d is beyond the launch grid limits", who, D.n);
     return hip_result(lrsa::launch_append_quant(D, Q, K, V, tokens, lens, counts, (hipStream_t)stream), who);
 }
@@ -591,6 +603,8 @@ int lrsa_cache_read_quant(const lrsa_params* p, const lrsa_quant_cache* c, const
     if (rows < 1) return fail(LRSA_ERR_INVALID_ARG, "%s: rows must be >= 1", who);
     if (!K || !V || !lens) return fail(LRSA_ERR_INVALID_ARG, "%s: K, V and lens must not be NULL", who);
     if (misaligned16(K) || misaligned16(V)) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
+    if (K == V) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be two", who);
+    if ((rc = check_written(who, D, D.ks)) != LRSA_OK) return rc;
     if (!lrsa::read_quant_grid_fits(D, rows)) return fail(LRSA_ERR_UNSUPPORTED, "%s: rows %d are beyond the launch grid limits", who, rows);
     return hip_result(lrsa::launch_read_quant(D, Q, lens, rows, first, K, V, (hipStream_t)stream), who);
 }
@@ -631,6 +645,7 @@ int lrsa_cache_evict_quant(const lrsa_params* p, const lrsa_quant_cache* c, cons
     if ((rc = check_evict(who, D, max_len, budget, recent)) != LRSA_OK) return rc;
     if (Q.K == N.K || Q.V == N.V || Q.K == N.V || Q.V == N.K || N.K == N.V || Q.Ks == N.Ks || Q.Vs == N.Vs || Q.Ks == N.Vs || Q.Vs == N.Ks || N.Ks == N.Vs)
         return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must not be the old one", who);
+    if ((rc = check_written(who, D, N)) != LRSA_OK) return rc;
     if (!lens || !lens_o || lens == lens_o) return fail(LRSA_ERR_INVALID_ARG, "%s: lens and lens_o must be two arrays", who);
     if ((rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
     if ((rc = check_ws_bytes(who, lrsa::cache_evict_ws_bytes(D, budget), ws, ws_bytes)) != LRSA_OK) return rc;

@@ -648,9 +648,9 @@ static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
     // one: then several rounds, of few more slices than units.  8 KV heads, 64 requests of 2048 rows: units + 256 55 us, + 512 58,
     // + 768 67, + 2048 71; 33 of 4096: 80, 70, 65, 70.
     // With few units of long bf16 rows, one workgroup per CU keeps enough loads in flight, and half as many slices are joined: 8 KV heads, bf16,
-    // d 128, 4 columns, 256 and 512 workgroups: 1 request of 16K rows 16.1 us and 18.7, of 128K 50.7 and 54.0, 4 of 20K 35.0 and 38.5, of 11K
-    // to 32K each 30.2 and 31.0, but 8 of those 76.5 and 75.1; 20 columns: 1 of 20K 21.6 and 23.7, 4 of 40K 90 and 84; d 64, 4 of
-    // 40K 39.9 and 37.2; fp32 71 and 64.5.
+    // d 128, 4 columns, 256 and 512 workgroups: 1 request of 16K rows 15.9 us and 17.6, of 128K 50.5 and 54.1, 4 of 40K 59.7 and 62.5, of
+    // 13K to 40K each 50.3 and 51.3, but 8 of 11K to 32K 76.5 and 75.1; 20 columns: 1 of 16K 20.4 and 23.1, of 128K 77.9 and 74.7, 4 of 40K
+    // 90 and 84; d 64, 4 of 40K 39.9 and 37.2; fp32 71 and 64.5.
     const bool few = D.dtype == 1 && D.d == 128 && units <= (D.G * tokens <= 16 ? 32 : 8);
     const int64_t most = few ? 256 : units <= 256 ? 512 : units + 512;
     const int64_t tiles = (int64_t(max_len) + QT - 1) / QT, fine = units * ((tiles + DEC_WAVES - 1) / DEC_WAVES);
@@ -678,8 +678,8 @@ bool decode_quant_grid_fits(const Dims& D, int tokens, int max_len) {
 }
 
 // One workgroup per unit, or slices?  Heads of 64: one, always (1 request of 1024 rows 8.8 us, slices 12.0; 64 of 1024 16.7, 30.3).
-// Heads of 128 have twice the bytes: one where it is short (12 heads on 2, 100 rows: 8.7, 12.5) or where units fill the card (16 requests of 1000 rows: 15.9, 17.5; 64 of 1024: 31.9, 51.3), slices else (1 request of
-// 1024 rows: 13.8, 12.0).
+// Heads of 128 have twice the bytes: one where it is short (12 heads on 2, 100 rows: 8.7, 12.5) or where units fill the card (16 requests
+// of 1000 rows: 13.6, 17.5; 64 of 1024: 32.2, 51.3), slices else (1 request of 1024 rows: 13.8, 12.0).
 static bool short_cache(const Dims& D, int cols, int max_len) {
     return cols <= 16 && max_len <= SHORT_ROWS && (D.d == 64 || max_len <= SHORT_ROWS / 2 || int64_t(D.B) * D.Hkv >= 128);
 }

@@ -193,6 +193,27 @@ def test_quant_calls_refuse():
     _refused(evict(nb=16), -1, "workspace")
 
 
+def test_rows_that_are_written_must_not_be_shared():
+    """Broadcast caches may be read, not written; K and V of a cache that is written are two."""
+    L, p = lrsa.lib(), _p()
+    r, out = ctypes.byref(p), ctypes.c_int32(-7)
+    shared = _p()
+    good = ctypes.byref(_c())
+    for st in ((0, 12800, 128), (25600, 0, 128)):
+        c = ctypes.byref(_c(stride=st))
+        _refused(L.lrsa_cache_append_quant(r, c, FAKE, FAKE, 1, FAKE, None, None), -1, "share")
+        c = ctypes.byref(_c(FAKE4, FAKE3, FAKE2, FAKE, stride=st))
+        _refused(L.lrsa_cache_evict_quant(r, good, None, FAKE, FAKE, 100, 50, 1, c, None, FAKE2, FAKE2, FAKE, 1 << 30, None), -1, "share")
+        shared.kv_stride[:] = st
+        s = ctypes.byref(shared)
+        _refused(L.lrsa_cache_read_quant(s, good, FAKE, 1, None, FAKE, FAKE2, None), -1, "share")
+        _refused(L.lrsa_cache_evict(s, FAKE, FAKE, None, FAKE, 100, 50, 10, FAKE2, FAKE3, None, FAKE2, ctypes.byref(out), FAKE, 1 << 30, None), -1, "share")
+    _refused(L.lrsa_cache_append_quant(r, ctypes.byref(_c(V=FAKE)), FAKE, FAKE, 1, FAKE, None, None), -1, "must be two")
+    _refused(L.lrsa_cache_append_quant(r, ctypes.byref(_c(Vs=FAKE3)), FAKE, FAKE, 1, FAKE, None, None), -1, "must be two")
+    _refused(L.lrsa_cache_read_quant(r, good, FAKE, 1, None, FAKE, FAKE, None), -1, "must be two")
+    assert out.value == -7
+
+
 def test_workspaces_for_a_longer_cache_are_enough_for_a_shorter_one():
     for kw in (dict(B=1, Hq=12, Hkv=2), dict(B=16, Hq=32, Hkv=8), dict(B=1, Hq=1, Hkv=1), dict(B=20, Hq=64, Hkv=8, dtype=torch.float32), dict(B=8, Hq=32, Hkv=8, d=64)):
         p = _p(cap=50000, **kw)
