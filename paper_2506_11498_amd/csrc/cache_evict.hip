@@ -371,7 +371,8 @@ __device__ __forceinline__ int select_chunk(const Dims& D, const EvictArgs& E, i
         E.acc_o[at + i] = 0.0f;
     return rows;
 }
-// strides and rows in 16-byte pieces
+// strides and rows in 16-byte pieces.  Through the caches, which hold as much as moves here, so that the next attention finds it there: 32
+// heads, 2048 of 4501 rows, 17.7 us, and 33.1 with the attention; past them 20.5 and 38.5.
 __global__ __launch_bounds__(EVICT_THREADS) void k_evict_short(Dims D, EvictArgs E, const uint4* __restrict__ K, const uint4* __restrict__ V, int pieces,
                                                                int chunk, uint4* __restrict__ Ko, uint4* __restrict__ Vo) {
     __shared__ int32_t list[SHORT_CHUNK];
@@ -382,13 +383,13 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_evict_short(Dims D, EvictArgs
     for (int i = threadIdx.x / pieces; i < rows; i += 2 * step) {
         const int j = min(i + step, rows - 1);               // the last row twice rather than loads in a branch
         const int64_t a = at + list[i] * D.ks[2] + sub, c = at + list[j] * D.ks[2] + sub;
-        const uint4 k0 = stream_load(K + a), v0 = stream_load(V + a), k1 = stream_load(K + c), v1 = stream_load(V + c);
+        const uint4 k0 = K[a], v0 = V[a], k1 = K[c], v1 = V[c];
         uint4 *Kn = Ko + at + row0 * D.ks[2] + sub, *Vn = Vo + at + row0 * D.ks[2] + sub;
-        stream_store(Kn + i * D.ks[2], k0);
-        stream_store(Vn + i * D.ks[2], v0);
+        Kn[i * D.ks[2]] = k0;
+        Vn[i * D.ks[2]] = v0;
         if (i + step < rows) {
-            stream_store(Kn + j * D.ks[2], k1);
-            stream_store(Vn + j * D.ks[2], v1);
+            Kn[j * D.ks[2]] = k1;
+            Vn[j * D.ks[2]] = v1;
         }
     }
 }
@@ -424,7 +425,8 @@ static EvictArgs evict_args(const Dims& D, const int32_t* lens, int len, int bud
 
 // One launch where a workgroup has all keys of its unit in registers and every workgroup a CU of its own, so that the selections that are
 // made several times cost no time.  bf16, d 128, one launch and two: 8 heads, 4501 rows of which 2048 stay 12.4 and 15.5 us, 32 heads (256
-// workgroups) 21.0 and 22.3, 32 heads of which 6000 stay (384) 53 and 43; 8 bits, 4 heads, 8111 rows of
+// workgroups) 19.9 and 22.3, 64 heads (256, of 512 rows) 37 and 34, 256 heads, 500 of 1000 rows (256) 34 and 37, 32 heads of which 6000 stay
+// (384) 53 and 43; 8 bits, 4 heads, 8111 rows of
 // which 2048 stay, and reading them back, 16.4 and 18.7.
 static bool short_eviction(const Dims& D, int len, int rows, int chunk) {
     return len <= EVICT_SHORT && (int64_t(rows) + chunk - 1) / chunk * D.B * D.Hkv <= 256;
