@@ -425,9 +425,8 @@ static EvictArgs evict_args(const Dims& D, const int32_t* lens, int len, int bud
 
 // One launch where a workgroup has all keys of its unit in registers and every workgroup a CU of its own, so that the selections that are
 // made several times cost no time.  bf16, d 128, one launch and two: 8 heads, 4501 rows of which 2048 stay 12.4 and 15.5 us, 32 heads (256
-// workgroups) 19.9 and 22.3, 64 heads (256, of 512 rows) 37 and 34, 256 heads, 500 of 1000 rows (256) 34 and 37, 32 heads of which 6000 stay
-// (384) 53 and 43; 8 bits, 4 heads, 8111 rows of
-// which 2048 stay, and reading them back, 16.4 and 18.7.
+// workgroups) 19.9 and 22.3, 64 heads (256, of 512 rows) 37 and 34, 256 heads, 500 of 1000 rows (256) 34 and 37, 32 heads, 6000 of 8192 rows
+// (384) 53 and 43; 8 bits, 4 heads, 2048 of 8111 rows, and reading them back, 16.4 and 18.7.
 static bool short_eviction(const Dims& D, int len, int rows, int chunk) {
     return len <= EVICT_SHORT && (int64_t(rows) + chunk - 1) / chunk * D.B * D.Hkv <= 256;
 }
