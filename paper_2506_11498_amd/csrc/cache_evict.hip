@@ -323,7 +323,9 @@ __device__ __forceinline__ void move_quant_rows(const QuantDims& Q, const QuantD
     for (int p = 0; p < PASSES; ++p) {
         const int r = p * RPP + rg;
         if (r >= rows) continue;
-        const float ratio = scale[p] * (1.0f / sh.scale[r >> N.log_block]);      // exact for powers of two
+        // Exact for powers of two.  Beyond 2^127 where a row of zeros leaves a large scale for a block of zeros: a number all the same, for 0 * ratio
+        // is to be 0 (a code that is not zero asks for 2^18 at most)
+        const float ratio = fminf(scale[p] * (1.0f / sh.scale[r >> N.log_block]), 0x1p127f);
         uint4 c = codes[p];
         if (ratio != 1.0f) {
             float lo[8], hi[8];
