@@ -311,7 +311,8 @@ int lrsa_cache_evict(const lrsa_params *p, const void *Kc, const void *Vc, const
  *
  * A row's value is code * scale of its block.  The scale is a power of two: the least 2^e, e >= -120, by which the block's
  * largest magnitude does not exceed the largest code (int8: 127, e4m3: 448); the code is the nearest one to value / scale, ties
- * to even.  Values are then exact in bf16, and rows that change their block keep their value unless the new block's scale is
+ * to even.  Magnitudes above 127 * 2^121 (int8) or 240 * 2^120 (e4m3), the largest values that are finite in fp32 and bf16, count as
+ * these.  Values are then exact in bf16, and rows that change their block keep their value unless the new block's scale is
  * too coarse for it.  A row that holds NaN or infinities gives its block an unspecified finite scale and finite codes; other
  * blocks do not change.  (The attention call takes any finite scales with which the logits stay below 1e29, and int8 codes down to -128.)
  *

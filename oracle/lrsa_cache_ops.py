@@ -8,6 +8,7 @@ from __future__ import annotations
 import numpy as np
 
 TOP = {"int8": 127.0, "e4m3": 448.0}
+LARGEST = {"int8": 127 * 2.0 ** 121, "e4m3": 240 * 2.0 ** 120}      # values: the next ones are 2^128
 
 
 def e4m3_value(code: int) -> float:
@@ -42,7 +43,7 @@ def encode(y: np.ndarray, fmt: str) -> np.ndarray:
 
 
 def scale_for(top: float, fmt: str) -> float:
-    s = 2.0 ** -120
+    top, s = min(top, LARGEST[fmt]), 2.0 ** -120
     while top > TOP[fmt] * s:
         s *= 2.0
     return s
@@ -55,7 +56,7 @@ def append(codes, scales, block, fmt, length, new):
     end = length + len(new)
     for j in range(length // block, -(-end // block) if len(new) else 0):
         a, b = max(j * block, length), min((j + 1) * block, end)
-        x = new[a - length:b - length]
+        x = np.clip(new[a - length:b - length], -LARGEST[fmt], LARGEST[fmt])
         s = scale_for(np.abs(x).max(), fmt)
         if a > j * block:                              # older rows in front
             old = scales[j]

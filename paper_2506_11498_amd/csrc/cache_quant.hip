@@ -48,7 +48,13 @@ __global__ __launch_bounds__(QUANT_THREADS) void k_append_quant(Dims D, QuantDim
     for (int p = 0; p < PASSES; ++p)
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[p][i]));
-    const float s = fmaxf(quant_scale<FMT>(block_max<QUANT_THREADS>(top, sm)), before);
+    top = block_max<QUANT_THREADS>(top, sm);
+    if (top > QUANT_LARGEST<FMT>)
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[p][i] = __builtin_amdgcn_fmed3f(v[p][i], -QUANT_LARGEST<FMT>, QUANT_LARGEST<FMT>);
+    const float s = fmaxf(quant_scale<FMT>(top), before);
     const float inv = 1.0f / s;
     if (s > before) {
         for (int r = rg; r < r0; r += RPP) {

@@ -5,6 +5,8 @@
 //   code   c = round(x / s), ties to even: a whole number in [-127, 127], or the nearest e4m3 number (4 bits exponent of
 //          bias 7, 3 bits fraction, no infinities)
 //   value  c s
+// Magnitudes above 127 * 2^121 (int8) or 240 * 2^120 (e4m3), the largest values that are numbers of 32 bits, count as these: the next code's
+// or the next scale's value would be 2^128.
 // Because s is a power of two, x / s is exact, so the code is that of the definition bit for bit; c has at most 8
 // significant bits, so the value is exact in bf16; and a code that moves to a block of another scale keeps its value unless
 // the new scale is too coarse for it (int8: some low bits; e4m3: subnormals only).  With s = max / Q the values would be
@@ -26,11 +28,12 @@ struct QuantDims {
 };
 
 #if defined(__HIPCC__)
+template <int FMT> constexpr float QUANT_LARGEST = FMT == QUANT_INT8 ? 0x1.fcp127f : 0x1.ep127f;
 template <int FMT>
 __device__ __forceinline__ float quant_scale(float top) {
     constexpr int UP = FMT == QUANT_INT8 ? 6 : 8;                             // Q = 1.984375 * 2^6, 1.75 * 2^8
     constexpr uint32_t FRAC = FMT == QUANT_INT8 ? 0x7e0000u : 0x600000u;
-    const uint32_t u = __float_as_uint(top);
+    const uint32_t u = __float_as_uint(fminf(top, QUANT_LARGEST<FMT>));
     const int e = max(int(u >> 23) - UP + ((u & 0x7fffffu) > FRAC ? 1 : 0), 127 - 120);
     return __uint_as_float(uint32_t(e) << 23);
 }

@@ -237,3 +237,15 @@ def test_the_binding_refuses_other_layouts():
     p = _p(cap=64)
     with pytest.raises((ValueError, RuntimeError, AssertionError)):       # tensors of the CPU
         lrsa.lrsa_cache_append_quant(p, c, torch.zeros((2, 2, 1, 128), dtype=torch.bfloat16), torch.zeros((2, 2, 1, 128), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_the_largest_values_are_finite_and_the_nearest_there_are(fmt):
+    """At the end of the range: the codes of the largest scale whose values are numbers of 32 bits and of bf16, the nearest one of them each."""
+    big, scale = ops.LARGEST[fmt], 2.0 ** (121 if fmt == "int8" else 120)
+    assert big == float(np.float32(big)) == float(torch.tensor(big).bfloat16()) and ops.scale_for(3.4028234663852886e38, fmt) == scale
+    numbers = np.array([v * scale for v in ops.decode(np.arange(256, dtype=np.uint8), fmt) if abs(v * scale) <= big])
+    x = np.linspace(0.95 * 2.0 ** 127, 3.4028234663852886e38, 640).reshape(10, 64) * np.where(np.arange(64) % 3, 1, -1)
+    codes, scales = ops.append(np.zeros((16, 64), np.uint8), np.ones(1), 16, fmt, 0, x)
+    got = ops.values(codes, scales, 16, fmt)[:10]
+    assert np.array_equal(np.abs(got - x), np.abs(x[..., None] - numbers).min(-1)) and scales[0] == scale and np.abs(got).max() == big

@@ -1,4 +1,4 @@
-"""The cache in 8 bits at the ends of its range: rows of zeros out of blocks with large scales.  Oracle as in test_gpu_cache_quant.py.
+"""The cache in 8 bits at the ends of its range: rows of zeros out of blocks with large scales, the largest numbers.  Oracle as in test_gpu_cache_quant.py.
 """
 import numpy as np
 import pytest
@@ -7,7 +7,7 @@ import torch
 import paper_2506_11498_amd as lrsa
 from oracle import lrsa_cache_ops as ops
 from test_gpu_cache_quant import CODES, host, i32
-from test_gpu_cache_weights import DEV, params
+from test_gpu_cache_weights import DEV, DT, params
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,36 @@ def test_rows_of_zeros_stay_zero_whatever_the_scale_that_they_leave(fmt, d, n, b
     for z in range(2):
         assert np.array_equal(got[2 + z][0, 0, :len(want)].astype(np.float64), want)
         assert np.array_equal(ops.decode(got[z][0, 0, :budget], fmt), ops.decode(codes, fmt))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,block", [("f32", 16), ("bf16", 32)])
+def test_finite_values_stay_finite(fmt, dtype, block):
+    """Rows up to the largest finite number: codes and scales of the definition, and every value that is read back is finite and off by at
+    most half a step of its scale, or is the largest one where the row's is beyond it.  The same after a move to another cache, and in attention over one row."""
+    T, d, big, least = DT[dtype], 64, ops.LARGEST[fmt], 2.0 ** 118
+    most = torch.finfo(T).max
+    x = torch.linspace(0, 1, block * d).view(block, d).double() * (most - least) + least
+    x[::2] *= -1
+    x[-1, -1] = most
+    x = torch.cat([x, x.clamp(-big, big), x * 2.0 ** -1]).to(T).clamp(-most, most)[None, None]      # the first block above the largest value, the second just below
+    n = x.shape[2]
+    cache, other = (lrsa.QuantCache.empty(1, 1, n, d, CODES[fmt], block, DEV) for _ in range(2))
+    p = params(1, 1, 1, n, d, x.stride(), T)
+    lrsa.lrsa_cache_append_quant(p, cache, x.to(DEV), x.to(DEV), i32([0]))
+    codes, scales = ops.append(np.zeros((n, d), np.uint8), np.ones(3), block, fmt, 0, x[0, 0].double().numpy())
+    got = host(cache)
+    assert np.array_equal(got[2][0, 0].astype(np.float64), scales)
+    assert np.array_equal(ops.decode(got[0][0, 0], fmt), ops.decode(codes, fmt))
+    Kr, Vr = lrsa.lrsa_cache_read_quant(p, cache, i32([n]), n)
+    r, want = Kr[0, 0].double().cpu().numpy(), x[0, 0].double().numpy()
+    assert np.all(np.isfinite(r)) and torch.equal(Kr, Vr)
+    step = scales.repeat(block)[:, None] * (1.0 if fmt == "int8" else 2.0 ** -9)
+    kept = np.clip(want, -big, big)
+    assert np.all(np.abs(r - kept) <= step / 2 + (0.0 if fmt == "int8" else 2.0 ** -4) * np.abs(kept))
+    ao, lo = torch.empty((1, 1, n), device=DEV), i32([0])
+    lrsa.lrsa_cache_evict_quant(p, cache, None, torch.ones((1, 1, n), device=DEV), i32([n]), n, n, 0, other, None, ao, lo)
+    assert torch.equal(other.K.view(torch.uint8), cache.K.view(torch.uint8)) and torch.equal(other.V_scale, cache.V_scale)
+    # a cache of one row has a weight of one: V's values, whatever the logit
+    O, _ = lrsa.lrsa_decode_attn_quant(p, torch.zeros((1, 1, 1, d), dtype=T, device=DEV), cache, i32([1]), 1)
+    assert torch.equal(O[0, 0, 0], Vr[0, 0, 0])
