@@ -314,7 +314,8 @@ int lrsa_cache_evict(const lrsa_params *p, const void *Kc, const void *Vc, const
  * to even.  Magnitudes above 127 * 2^121 (int8) or 240 * 2^120 (e4m3), the largest values that are finite in fp32 and bf16, count as
  * these.  Values are then exact in bf16, and rows that change their block keep their value unless the new block's scale is
  * too coarse for it.  A row that holds NaN or infinities gives its block an unspecified finite scale and finite codes; other
- * blocks do not change.  (The attention call takes any finite scales with which the logits stay below 1e29, and int8 codes down to -128.)
+ * blocks do not change.  (The attention call takes any finite scales with which the logits stay below 1e29 and the values of
+ * V summed over a cache's rows below 3e38, and int8 codes down to -128.)
  *
  * In these calls p->seq is cap, the rows that the cache has room for; dtype is that of q, O and of the rows K, V given to
  * lrsa_cache_append_quant and taken by lrsa_cache_read_quant, which kv_stride describes; q_stride is not used.  Every sequence

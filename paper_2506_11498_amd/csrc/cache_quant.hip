@@ -227,9 +227,14 @@ __device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantRow
     }
 }
 
-// NG groups of 16 columns.  seen: rows from the lane's first one on that its column sees; ACC: the logits go to `out`
+// NG groups of 16 columns.  seen: rows from the lane's first one on that its column sees; ACC: the logits go to `out`.
+// o is in units of 2^(unit - 127), the power of two of the largest scale of V so far (1 at most, so that no weight gets smaller for it): a weight
+// times a scale of 2^-110 or less has terms below the least bf16 number (2^-133), and would keep 14 bits at 2^-120.  A tile's scales are
+// the same in all lanes (each 16 rows share one), so the unit is a scalar.  It costs 0.2 us in short caches, nothing in long ones.
+constexpr uint32_t LEAST_UNIT = 127 - 120;
+__device__ __forceinline__ float unit_value(uint32_t unit) { return __uint_as_float(unit << 23); }
 template <int DH, int FMT, int TERMS, bool ACC, int NG>
-__device__ __forceinline__ void use_quant_tile(float (&m)[NG], float (&l)[NG], f32x4 (&o)[NG][DH / 16], const QuantTile<DH>& t,
+__device__ __forceinline__ void use_quant_tile(float (&m)[NG], float (&l)[NG], f32x4 (&o)[NG][DH / 16], uint32_t& unit, const QuantTile<DH>& t,
                                                const bf16x8 (&qf)[NG][TERMS][DH / 32], const int (&seen)[NG], float c2, LogitBuffer (&out)[NG]) {
     f32x4 s[NG][2];
 #pragma unroll
@@ -249,6 +254,17 @@ __device__ __forceinline__ void use_quant_tile(float (&m)[NG], float (&l)[NG], f
                 for (int i = TERMS - 1; i >= 0; --i) s[g][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][i][kk], s[g][kb], 0, 0, 0);
         }
     const float c2s[2] = {c2 * t.ks[0], c2 * t.ks[1]};
+    const float top = __builtin_amdgcn_fmed3f(fmaxf(fabsf(t.vs[0]), fabsf(t.vs[1])), unit_value(LEAST_UNIT), 1.0f);
+    const uint32_t now = max(unit, uint32_t(__builtin_amdgcn_readfirstlane(__float_as_uint(top))) >> 23);
+    if (now != unit) {
+        const float a = unit_value(127 + unit - now);
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int e = 0; e < DH / 16; ++e) o[g][e] *= a;
+        unit = now;
+    }
+    const float vs[2] = {t.vs[0] * unit_value(254 - unit), t.vs[1] * unit_value(254 - unit)};
     bf16x8 term[NG][3];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -276,7 +292,7 @@ __device__ __forceinline__ void use_quant_tile(float (&m)[NG], float (&l)[NG], f
         for (int j = 0; j < 8; ++j) {
             const float e = __builtin_amdgcn_exp2f(p[j] - m[g]);
             ps += e;
-            w[j] = e * t.vs[j >> 2];
+            w[j] = e * vs[j >> 2];
         }
         l[g] += ps;
 #pragma unroll
@@ -374,6 +390,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
         const int g0 = c0 + CW * (wave % groups), gn = min(CW, cols - g0);      // of this wave: none where not positive
         float m[NG], l[NG];
         f32x4 o[NG][CPL];
+        uint32_t unit = LEAST_UNIT;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             m[g] = NO_WEIGHT;
@@ -411,7 +428,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
                 int seen[NG];
 #pragma unroll
                 for (int g = 0; g < NG; ++g) seen[g] = vis[g] - r;
-                use_quant_tile<DH, FMT, TERMS, ACC, NG>(m, l, o, t, qf, seen, c2, out);
+                use_quant_tile<DH, FMT, TERMS, ACC, NG>(m, l, o, unit, t, qf, seen, c2, out);
             };
             for (;;) {
                 load(B, r + step);
@@ -439,7 +456,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
 #pragma unroll
                     for (int e = 0; e < CPL; e += 4)
                         *reinterpret_cast<f32x4*>(&sBuf[wave][cw * LROW + (4 * q4 + i) * CPL + e]) =
-                            f32x4{o[g][e][i], o[g][e + 1][i], o[g][e + 2][i], o[g][e + 3][i]};
+                            f32x4{o[g][e][i], o[g][e + 1][i], o[g][e + 2][i], o[g][e + 3][i]} * unit_value(unit);
             }
         }
         __syncthreads();
@@ -482,6 +499,7 @@ __global__ __launch_bounds__(64 * SHORT_WAVES) void k_decode_quant_short(Dims D,
     const int64_t col0 = int64_t(bh) * cols;
     float m[1] = {NO_WEIGHT}, l[1] = {0.0f};
     f32x4 o[1][CPL];
+    uint32_t unit = LEAST_UNIT;
 #pragma unroll
     for (int e = 0; e < CPL; ++e) o[0][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     int r = wave * QT;
@@ -505,7 +523,7 @@ __global__ __launch_bounds__(64 * SHORT_WAVES) void k_decode_quant_short(Dims D,
         if constexpr (ACC) out[0] = logit_buffer(sLogit[wave], LOGITS, nullptr, 0, cols, 0);      // room for all of the wave's tiles
         auto use = [&](const QuantTile<DH>& t) {
             const int seen[1] = {vis - r};
-            use_quant_tile<DH, FMT, TERMS, ACC, 1>(m, l, o, t, qf, seen, c2, out);
+            use_quant_tile<DH, FMT, TERMS, ACC, 1>(m, l, o, unit, t, qf, seen, c2, out);
         };
         for (;;) {
             load(B0, r + STEP);
@@ -526,7 +544,8 @@ __global__ __launch_bounds__(64 * SHORT_WAVES) void k_decode_quant_short(Dims D,
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < CPL; e += 4)
-                *reinterpret_cast<f32x4*>(&sO[wave][c * LROW + (4 * q4 + i) * CPL + e]) = f32x4{o[0][e][i], o[0][e + 1][i], o[0][e + 2][i], o[0][e + 3][i]};
+                *reinterpret_cast<f32x4*>(&sO[wave][c * LROW + (4 * q4 + i) * CPL + e]) =
+                    f32x4{o[0][e][i], o[0][e + 1][i], o[0][e + 2][i], o[0][e + 3][i]} * unit_value(unit);
     }
     __syncthreads();
     const int waves = max(1, min(SHORT_WAVES, (len + QT - 1) / QT));         // those that had a tile

@@ -1,4 +1,5 @@
-"""The cache in 8 bits at the ends of its range: rows of zeros out of blocks with large scales, the largest numbers.  Oracle as in test_gpu_cache_quant.py.
+"""The cache in 8 bits at the ends of its range: rows of zeros out of blocks with large scales, the largest numbers, small
+values in attention.  Oracle as in test_gpu_cache_quant.py.
 """
 import numpy as np
 import pytest
@@ -7,7 +8,7 @@ import torch
 import paper_2506_11498_amd as lrsa
 from oracle import lrsa_cache_ops as ops
 from test_gpu_cache_quant import CODES, host, i32
-from test_gpu_cache_weights import DEV, DT, params
+from test_gpu_cache_weights import DEV, DT, close_attention, params
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +72,50 @@ def test_finite_values_stay_finite(fmt, dtype, block):
     # a cache of one row has a weight of one: V's values, whatever the logit
     O, _ = lrsa.lrsa_decode_attn_quant(p, torch.zeros((1, 1, 1, d), dtype=T, device=DEV), cache, i32([1]), 1)
     assert torch.equal(O[0, 0, 0], Vr[0, 0, 0])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,B,Hkv,G,T,n", [
+    ("f32", 128, 1, 1, 4, 1, 5), ("f32", 64, 2, 2, 2, 3, 700), ("bf16", 128, 1, 2, 4, 1, 3000), ("f32", 128, 1, 1, 20, 1, 2500), ("f32", 64, 4, 8, 4, 5, 21000),
+    ("bf16", 128, 4, 8, 4, 5, 21000),
+])
+def test_attention_keeps_its_bits_where_values_are_small(fmt, dtype, d, B, Hkv, G, T, n):
+    """Scales of V that are 2^-k of others (powers of two, different ones along the cache) give outputs that are 2^-k of theirs, bit for bit: no
+    product, weight or sum has fewer bits there, as long as the outputs themselves are normal numbers."""
+    block = 16
+    g = torch.Generator(device=DEV).manual_seed(n + G)
+    raw = [torch.randint(0, 256, (B, Hkv, n, d), generator=g, device=DEV, dtype=torch.uint8) for _ in range(2)]
+    for r in raw:
+        r.bitwise_and_(0xbf if fmt == "e4m3" else 0xff)                          # e4m3: magnitudes below 2
+    nb = -(-n // block)
+    Ks = torch.exp2(torch.randint(-9, -5, (B, Hkv, nb), generator=g, device=DEV).float()) * (64 if fmt == "e4m3" else 1)
+    Vs = torch.exp2(torch.randint(0, 5, (B, Hkv, nb), generator=g, device=DEV).float())
+    q = torch.randn((B, Hkv * G, T, d), generator=g, device=DEV).to(DT[dtype])
+    p, lens = params(B, Hkv * G, Hkv, n, d, (Hkv * n * d, n * d, d, 1), DT[dtype]), i32([n - 3 * b for b in range(B)])
+    outs = []
+    for k in (8, 40, 104, 113):
+        cache = lrsa.QuantCache(*(r.view(CODES[fmt]) for r in raw), Ks, Vs * 2.0 ** -k, block)
+        outs.append(lrsa.lrsa_decode_attn_quant(p, q, cache, lens, n))
+        want = torch.ldexp(outs[0][0].double(), torch.tensor(8.0 - k, device=DEV)).to(DT[dtype])
+        normal = want.abs() >= torch.finfo(DT[dtype]).tiny
+        assert torch.equal(outs[-1][1], outs[0][1]) and bool((outs[-1][0] == want)[normal].all()) and float(normal.float().mean()) > 0.9
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_small_and_large_values_in_one_cache(fmt):
+    """V scales from the least to 2^60 in one cache; tokens that see the small ones alone, the large ones among them or first."""
+    d, block, n, G = 128, 16, 160, 4
+    g = torch.Generator().manual_seed(12)
+    raw = [torch.randint(0, 256, (1, 1, n, d), generator=g, dtype=torch.uint8) & (0xbf if fmt == "e4m3" else 0xff) for _ in range(2)]
+    q = torch.randn((1, G, 1, d), generator=g)
+    p = params(1, G, 1, n, d, (n * d, n * d, d, 1), torch.float32)
+    Ks = torch.full((1, 1, n // block), 2.0 ** -8 if fmt == "int8" else 0.5)
+    for order in ([-120, -118, -100, -80, -40, -20, 0, 3, 30, 60], [60, 30, 3, 0, -20, -40, -80, -100, -118, -120]):
+        Vs = torch.exp2(torch.tensor(order).float()).view(1, 1, -1)
+        cache = lrsa.QuantCache(*(r.to(DEV).view(CODES[fmt]) for r in raw), Ks.to(DEV), Vs.to(DEV), block)
+        for m in (1, 16, 20, 33, 100, 111, 160):
+            O, lse = lrsa.lrsa_decode_attn_quant(p, q.to(DEV), cache, i32([m]), n)
+            k, v = (ops.values(r[0, 0].numpy(), s[0, 0].numpy(), block, fmt)[:m] for r, s in zip(raw, (Ks, Vs)))
+            qs = q[0].double().numpy()
+            O_ref, lse_ref, _ = ops.attend(qs, k, v)
+            close_attention(O[0].double().cpu().numpy(), lse[0].double().cpu().numpy(), qs, k, v, O_ref, lse_ref, d ** -0.5, 2.0 ** -24)
