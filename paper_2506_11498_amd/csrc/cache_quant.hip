@@ -153,7 +153,7 @@ __device__ __forceinline__ int slice_tiles(const Dims& D, const SeqLens& L, cons
 // A wave takes 16 * NG columns.  If these are all, the 4 waves take the tiles in turn (SOLE): every code is read by one wave of the
 // chip, and past the caches (PAST) where the cache is as large as the Infinity Cache (256 MB), which would keep little of it until the next call.  8 KV
 // heads of 4 query heads, us per call on the same cache, through and past the caches: 40 MB 14.6 and 16.2, 159 MB 32.5 and 35.3, 269 MB
-// 47.6 and 51.9, 537 MB 102 and 95; on others in turn: 16.2 and 16.8, 37.8 and 36.5, 54.5 and 52.3, 102 and 95.  Where there are more, `groups` (2 or 4) waves take the same tile, so that its codes come from memory once, and
+// 47.6 and 51.9, 537 MB 102 and 95; on others in turn: 16.2 and 16.8, 37.8 and 36.5, 54.5 and 52.3, 102 and 95 (NG = 2: decode_quant_kernel).  Where there are more, `groups` (2 or 4) waves take the same tile, so that its codes come from memory once, and
 // beyond 4 times as many columns the slice is walked again.  NG = 2 halves the unpacking of codes, which bounds many columns (8 requests of
 // 32K rows, 20 columns: 107 us, with NG = 1 128; 64 columns: 171 and 212); it needs registers that fp32 queries of 128 channels do not
 // leave, and long walks.
@@ -709,6 +709,25 @@ static bool short_cache(const Dims& D, int cols, int max_len) {
     return cols <= 16 && max_len <= SHORT_ROWS && (D.d == 64 || max_len <= SHORT_ROWS / 2 || int64_t(D.B) * D.Hkv >= 128);
 }
 
+// Two groups of columns in one wave go past the caches by size like one group (17 to 32 columns; 8 KV heads of 4 query heads, 5 tokens, bf16,
+// us per call on the same cache, through and past the caches: d 128, 83 MB 34 and 37, 163 MB 46 and 52, 229 MB 55 and 61; on others in turn: 33
+// and 37, 48 and 52, 61 and 60; d 64, 86 to 204 MB the same, in turn 35 and 34, 62 and 61), but at any size where weights are accumulated: the
+// logits, 64 bytes or more per row, are then found in the caches when they are read again (d 64, 122 MB, on others in turn 87 and 80, on
+// the same cache 73 and 80; d 128, 229 MB 109 and 99, 96 and 99; 537 MB 249 and 238, 243 and 200).
+template <typename T, int DH, int FMT>
+static auto decode_quant_kernel(int cols, bool wide, bool past, bool acc) {
+    constexpr int MOST = MOST_GROUPS<T, DH>;
+    if (cols <= 16 && past) return acc ? k_decode_quant<T, DH, FMT, 1, true, true, true> : k_decode_quant<T, DH, FMT, 1, true, true, false>;
+    if (cols <= 16) return acc ? k_decode_quant<T, DH, FMT, 1, true, false, true> : k_decode_quant<T, DH, FMT, 1, true, false, false>;
+    if constexpr (MOST > 1)
+        if (wide) {
+            if (cols > 16 * MOST) return acc ? k_decode_quant<T, DH, FMT, MOST, false, false, true> : k_decode_quant<T, DH, FMT, MOST, false, false, false>;
+            if (acc) return k_decode_quant<T, DH, FMT, MOST, true, true, true>;
+            return past ? k_decode_quant<T, DH, FMT, MOST, true, true, false> : k_decode_quant<T, DH, FMT, MOST, true, false, false>;
+        }
+    return acc ? k_decode_quant<T, DH, FMT, 1, false, false, true> : k_decode_quant<T, DH, FMT, 1, false, false, false>;
+}
+
 template <typename T>
 static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void* q, int tokens, const int32_t* lens, int max_len, void* O, float* lse,
                                    const float* acc_in, float* acc_out, float decay, void* ws, hipStream_t st) {
@@ -742,28 +761,14 @@ static hipError_t run_decode_quant(const Dims& D, const QuantDims& Q, const void
         return hipGetLastError();
     }
     const bool past = int64_t(D.B) * D.Hkv * max_len * D.d * 2 >= PAST_BYTES;
-#define LRSA_DECODE_QUANT(DH_, FMT_, NG_, SOLE_, PAST_)                                                                                   \
-    LRSA_TIMED_LAUNCH("k_decode_quant", st,                                                                                               \
-                      (acc_out ? k_decode_quant<T, DH_, FMT_, NG_, SOLE_, PAST_, true> : k_decode_quant<T, DH_, FMT_, NG_, SOLE_, PAST_, false>), \
-                      dim3(P.grid), dim3(DEC_THREADS), 0, st, D, Q, (const T*)q, tokens, lens, max_len, P.s, seqs, part, logits, P.rows,   \
-                      P.pitch)
-#define LRSA_DECODE_QUANT_FMT(DH_, FMT_)                                                            \
-    if (A.cols <= 16 && past) LRSA_DECODE_QUANT(DH_, FMT_, 1, true, true);                          \
-    else if (A.cols <= 16) LRSA_DECODE_QUANT(DH_, FMT_, 1, true, false);                            \
-    else if (!P.wide) LRSA_DECODE_QUANT(DH_, FMT_, 1, false, false);                                \
-    else if (A.cols <= 16 * MOST) LRSA_DECODE_QUANT(DH_, FMT_, MOST, true, true);                   \
-    else LRSA_DECODE_QUANT(DH_, FMT_, MOST, false, false)
-#define LRSA_DECODE_QUANT_DH(FMT_)                                                                  \
-    if (D.d == 64) {                                                                                \
-        constexpr int MOST = MOST_GROUPS<T, 64>;                                                    \
-        LRSA_DECODE_QUANT_FMT(64, FMT_);                                                            \
-    } else {                                                                                        \
-        constexpr int MOST = MOST_GROUPS<T, 128>;                                                   \
-        LRSA_DECODE_QUANT_FMT(128, FMT_);                                                           \
+#define LRSA_DECODE_QUANT(DH_, FMT_)                                                                                                      \
+    LRSA_TIMED_LAUNCH("k_decode_quant", st, (decode_quant_kernel<T, DH_, FMT_>(A.cols, P.wide, past, acc_out != nullptr)), dim3(P.grid),   \
+                      dim3(DEC_THREADS), 0, st, D, Q, (const T*)q, tokens, lens, max_len, P.s, seqs, part, logits, P.rows, P.pitch)
+    if (Q.fmt == QUANT_INT8) {
+        if (D.d == 64) LRSA_DECODE_QUANT(64, QUANT_INT8); else LRSA_DECODE_QUANT(128, QUANT_INT8);
+    } else {
+        if (D.d == 64) LRSA_DECODE_QUANT(64, QUANT_E4M3); else LRSA_DECODE_QUANT(128, QUANT_E4M3);
     }
-    if (Q.fmt == QUANT_INT8) { LRSA_DECODE_QUANT_DH(QUANT_INT8) } else { LRSA_DECODE_QUANT_DH(QUANT_E4M3) }
-#undef LRSA_DECODE_QUANT_DH
-#undef LRSA_DECODE_QUANT_FMT
 #undef LRSA_DECODE_QUANT
     LRSA_TIMED_LAUNCH("k_quant_combine", st, k_quant_combine<T>, dim3(unsigned(rows + D.B * D.Hkv * chunks)), dim3(DEC_THREADS), 0, st, D, part, tokens,
                       lens, max_len, P.s, seqs, (T*)O, lse, A, rows, chunks);
