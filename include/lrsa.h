@@ -294,7 +294,8 @@ int lrsa_decode_attn_acc(const lrsa_params *p, const void *q, const void *Kc, co
  * budget - sink - recent rows between them with the largest acc stay (equal ones: the lowest first), per (batch, KV head), in
  * position order; a cache with fewer keeps all.  They go to ANOTHER cache of the same layout, which a program swaps with the
  * old one (one spare for all layers is enough); the old one is left as it was.
- *   Kc, Vc, Ko, Vo : [B, Hkv, cap, d_h] by kv_stride; cap = p->seq; Ko, Vo rows behind the new length are left as they were
+ *   Kc, Vc, Ko, Vo : [B, Hkv, cap, d_h] by kv_stride; cap = p->seq; Ko, Vo rows behind the new length are left as they were;
+ *                    rows do not share memory
  *   pos, pos_o     : [B, Hkv, cap] int32, contiguous, moved alike; both may be NULL
  *   acc            : [B, Hkv, cap] fp32, contiguous, any finite values             (device, read)
  *   acc_o          : like acc: the weights of the rows that stay, and ZERO in all rows behind them, so that rows appended
@@ -333,7 +334,8 @@ typedef struct {
 /* Rows lens[b] .. lens[b] + counts[b] - 1 of sequence b become the first counts[b] rows of K and V.  Where the first of them
  * falls into a block with older rows, that block's scale grows if it must and its older codes are rounded to the new scale.  Rows
  * that would lie at or behind cap are dropped; lens is not changed; codes behind the new rows are left as they were.
- * Sequences and heads of a cache that is written must not share rows (no stride of 0), and its K and V are two.
+ * Sequences, heads and rows of a cache that is written must not share memory (of the three strides, each steps over all that the
+ * next smaller one covers), and its K and V are two.
  *   K, V   : [B, Hkv, tokens, d_h] by kv_stride, dtype `dtype`                     (device, read)
  *   counts : [B] int32, 0 <= counts[b] <= tokens (others count as the nearer bound), or NULL: tokens of every sequence */
 int lrsa_cache_append_quant(const lrsa_params *p, const lrsa_quant_cache *c, const void *K, const void *V, int32_t tokens,
@@ -341,7 +343,8 @@ int lrsa_cache_append_quant(const lrsa_params *p, const lrsa_quant_cache *c, con
 
 /* Rows first[b] .. first[b] + rows - 1 of sequence b as values; rows before 0 and at or behind lens[b] are zero.
  *   first : [B] int32 or NULL: 0
- *   K, V  : [B, Hkv, rows, d_h] by kv_stride, dtype `dtype`                        (device, written) */
+ *   K, V  : [B, Hkv, rows, d_h] by kv_stride, dtype `dtype`; none of these rows share memory (as they would by the strides of
+ *           fewer rows)                                                           (device, written) */
 int lrsa_cache_read_quant(const lrsa_params *p, const lrsa_quant_cache *c, const int32_t *lens, int32_t rows, const int32_t *first,
                           void *K, void *V, void *stream);
 

@@ -486,7 +486,7 @@ def lrsa_cache_append_quant(p: LrsaParams, cache: QuantCache, K: torch.Tensor, V
 def lrsa_cache_read_quant(p: LrsaParams, cache: QuantCache, lens: torch.Tensor, rows: int, first: Optional[torch.Tensor] = None,
                           K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
     """Rows first[b] (None: 0) .. + rows of every sequence as values [B, Hkv, rows, d], zero at and behind lens[b]; returns (K, V), by
-    default of the strides that p.kv_stride gives."""
+    default of the strides that p.kv_stride gives (refused where they are made for fewer rows)."""
     index, dev, i32 = _here(lens), lens.device, torch.int32
     (B, _, Hkv, cap, d), dt, ks = _read(p)
     kv, st = (B, Hkv, rows, d), (*ks, 1)

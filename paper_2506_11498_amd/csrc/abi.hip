@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <utility>
 
 namespace {
 
@@ -505,15 +506,25 @@ int make_quant(const char* who, const lrsa::Dims& D, const lrsa_quant_cache* c, 
     return LRSA_OK;
 }
 
-// rows that a call writes: no two in one place
-int check_written(const char* who, const lrsa::Dims& D, const int64_t (&st)[3]) {
-    if ((D.B > 1 && st[0] == 0) || (D.Hkv > 1 && st[1] == 0))
-        return fail(LRSA_ERR_INVALID_ARG, "%s: sequences or heads share their rows (stride 0), which would be written", who);
+// rows that a call writes, `rows` per head, each d long: no two in one place.  Axes by their strides: each steps over all of the one below it
+int check_written(const char* who, const lrsa::Dims& D, const int64_t (&st)[3], int64_t rows) {
+    struct { int64_t n, st; } ax[3] = {{D.B, st[0]}, {D.Hkv, st[1]}, {rows, st[2]}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (ax[j].st > ax[j + 1].st) std::swap(ax[j], ax[j + 1]);
+    __int128 extent = D.d;
+    for (const auto& a : ax)
+        if (a.n > 1) {
+            if (a.st < extent)
+                return fail(LRSA_ERR_INVALID_ARG, "%s: with strides %lld, %lld, %lld (sequences, heads, rows) %lld rows per head share memory that would be written",
+                            who, (long long)st[0], (long long)st[1], (long long)st[2], (long long)rows);
+            extent += (__int128)a.st * (a.n - 1);
+        }
     return LRSA_OK;
 }
-int check_written(const char* who, const lrsa::Dims& D, const lrsa::QuantDims& Q) {
+int check_written(const char* who, const lrsa::Dims& D, const lrsa::QuantDims& Q, int64_t rows) {
     if (Q.K == Q.V || Q.Ks == Q.Vs) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V of the cache that is written must be two", who);
-    return check_written(who, D, Q.st);
+    return check_written(who, D, Q.st, rows);
 }
 
 int check_evict(const char* who, const lrsa::Dims& D, int32_t len, int32_t budget, int32_t recent) {
@@ -571,7 +582,7 @@ int lrsa_cache_evict(const lrsa_params* p, const void* Kc, const void* Vc, const
     if (misaligned16(Kc) || misaligned16(Vc) || misaligned16(Ko) || misaligned16(Vo))
         return fail(LRSA_ERR_INVALID_ARG, "%s: Kc, Vc, Ko and Vo must be 16-byte aligned", who);
     if (Ko == Kc || Vo == Vc || Ko == Vc || Vo == Kc || Ko == Vo) return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must not be the old one", who);
-    if ((rc = check_written(who, D, D.ks)) != LRSA_OK || (rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
+    if ((rc = check_written(who, D, D.ks, budget)) != LRSA_OK || (rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
     if ((rc = check_ws_bytes(who, lrsa::cache_evict_ws_bytes(D, budget), ws, ws_bytes)) != LRSA_OK) return rc;
     rc = hip_result(lrsa::launch_cache_evict(D, Kc, Vc, pos, acc, len, budget, recent, Ko, Vo, pos_o, acc_o, ws, (hipStream_t)stream), who);
     if (rc == LRSA_OK) *len_out = len < budget ? len : budget;
@@ -588,7 +599,7 @@ int lrsa_cache_append_quant(const lrsa_params* p, const lrsa_quant_cache* c, con
     if (tokens < 1) return fail(LRSA_ERR_INVALID_ARG, "%s: tokens must be >= 1", who);
     if (!K || !V || !lens) return fail(LRSA_ERR_INVALID_ARG, "%s: K, V and lens must not be NULL", who);
     if (misaligned16(K) || misaligned16(V)) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
-    if ((rc = check_written(who, D, Q)) != LRSA_OK) return rc;
+    if ((rc = check_written(who, D, Q, D.n)) != LRSA_OK) return rc;
     if (!lrsa::grid_fits(Q.nb, 256)) return fail(LRSA_ERR_UNSUPPORTED, "%s: cap %d is beyond the launch grid limits", who, D.n);
     return hip_result(lrsa::launch_append_quant(D, Q, K, V, tokens, lens, counts, (hipStream_t)stream), who);
 }
@@ -604,7 +615,7 @@ int lrsa_cache_read_quant(const lrsa_params* p, const lrsa_quant_cache* c, const
     if (!K || !V || !lens) return fail(LRSA_ERR_INVALID_ARG, "%s: K, V and lens must not be NULL", who);
     if (misaligned16(K) || misaligned16(V)) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be 16-byte aligned", who);
     if (K == V) return fail(LRSA_ERR_INVALID_ARG, "%s: K and V must be two", who);
-    if ((rc = check_written(who, D, D.ks)) != LRSA_OK) return rc;
+    if ((rc = check_written(who, D, D.ks, rows)) != LRSA_OK) return rc;
     if (!lrsa::read_quant_grid_fits(D, rows)) return fail(LRSA_ERR_UNSUPPORTED, "%s: rows %d are beyond the launch grid limits", who, rows);
     return hip_result(lrsa::launch_read_quant(D, Q, lens, rows, first, K, V, (hipStream_t)stream), who);
 }
@@ -645,7 +656,7 @@ int lrsa_cache_evict_quant(const lrsa_params* p, const lrsa_quant_cache* c, cons
     if ((rc = check_evict(who, D, max_len, budget, recent)) != LRSA_OK) return rc;
     if (Q.K == N.K || Q.V == N.V || Q.K == N.V || Q.V == N.K || N.K == N.V || Q.Ks == N.Ks || Q.Vs == N.Vs || Q.Ks == N.Vs || Q.Vs == N.Ks || N.Ks == N.Vs)
         return fail(LRSA_ERR_INVALID_ARG, "%s: the new cache must not be the old one", who);
-    if ((rc = check_written(who, D, N)) != LRSA_OK) return rc;
+    if ((rc = check_written(who, D, N, budget)) != LRSA_OK) return rc;
     if (!lens || !lens_o || lens == lens_o) return fail(LRSA_ERR_INVALID_ARG, "%s: lens and lens_o must be two arrays", who);
     if ((rc = check_evict_lists(who, pos, acc, pos_o, acc_o)) != LRSA_OK) return rc;
     if ((rc = check_ws_bytes(who, lrsa::cache_evict_ws_bytes(D, budget), ws, ws_bytes)) != LRSA_OK) return rc;

@@ -249,3 +249,37 @@ def test_the_largest_values_are_finite_and_the_nearest_there_are(fmt):
     codes, scales = ops.append(np.zeros((16, 64), np.uint8), np.ones(1), 16, fmt, 0, x)
     got = ops.values(codes, scales, 16, fmt)[:10]
     assert np.array_equal(np.abs(got - x), np.abs(x[..., None] - numbers).min(-1)) and scales[0] == scale and np.abs(got).max() == big
+
+
+def test_rows_that_overlap_by_their_strides_are_not_written():
+    """Strides that were made for fewer rows, or heads less than a row apart; layouts whose axes come in another order are written."""
+    L, p = lrsa.lib(), _p()
+    r, out = ctypes.byref(p), ctypes.c_int32(-7)
+    good, other = ctypes.byref(_c()), _p()
+
+    def read(rows, st):
+        other.kv_stride[:] = st
+        return L.lrsa_cache_read_quant(ctypes.byref(other), good, FAKE, rows, None, FAKE, FAKE2, None)
+
+    def evict(st, budget=50):
+        other.kv_stride[:] = st
+        return L.lrsa_cache_evict(ctypes.byref(other), FAKE, FAKE, None, FAKE, 100, budget, 10, FAKE2, FAKE3, None, FAKE2, ctypes.byref(out), FAKE, 16, None)
+    # one row per head, taken for a call of more (the second head's first row is the first one's second)
+    for rows, st in ((2, (256, 128, 128)), (64, (256, 128, 128)), (9, (2048, 1024, 128)), (2, (128, 1024, 128)), (5, (512, 128, 256)), (3, (1024, 8, 128)),
+                     (3, (128, 4096, 248))):
+        _refused(read(rows, st), -1, "share")
+    for st in ((12800, 6272, 128), (6400, 6400, 128), (12672, 128, 256), (25600, 64, 128)):
+        _refused(evict(st), -1, "share")
+        _refused(L.lrsa_cache_append_quant(r, ctypes.byref(_c(stride=st)), FAKE, FAKE, 1, FAKE, None, None), -1, "share")
+        _refused(L.lrsa_cache_evict_quant(r, good, None, FAKE, FAKE, 100, 50, 1, ctypes.byref(_c(FAKE4, FAKE3, FAKE2, FAKE, stride=st)), None, FAKE2, FAKE2, FAKE,
+                                          1 << 30, None), -1, "share")
+    # layouts that are: refused for another reason, which is looked for later
+    for st in ((50 * 256, 128, 256), (50 * 128, 50 * 256, 128), (128, 50 * 256, 256), (128, 256, 512), (2 ** 50, 2 ** 40, 2 ** 20), (2 ** 60, 128, 2 ** 50)):
+        _refused(evict(st), -1, "workspace")
+    for st in ((2 ** 50, 2 ** 42, 128), (128, 256, 512), (2 ** 60, 128, 256), (128, 2 ** 42, 264)):
+        _refused(read(2 ** 31 - 1, st), -2, "grid")
+    # axes of length one have any stride
+    other = _p(B=1, Hkv=1)
+    _refused(read(2 ** 31 - 1, (0, 0, 128)), -2, "grid")
+    _refused(evict((0, 8, 128)), -1, "workspace")
+    assert out.value == -7
