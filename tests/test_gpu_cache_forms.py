@@ -1,4 +1,5 @@
-"""The inference-cache calls in forms that other tests leave out: 17 to 32 columns over caches larger than the GPU's.
+"""The inference-cache calls in forms that other tests leave out: 17 to 32 columns over caches larger than the GPU's, weights that are followed through
+evictions.
 Oracle and tolerances as in test_gpu_cache_weights.py.
 """
 import numpy as np
@@ -39,3 +40,49 @@ def test_two_groups_of_columns(fmt, dtype, d, n):
         eps = close_attention(O[b, hs].double().cpu().numpy(), lse[b, hs].double().cpu().numpy(), qs, K, V, O_ref, lse_ref, d ** -0.5,
                               2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
         assert np.all(np.abs(out[b, h, :m].double().cpu().numpy() - w) <= 2 * eps * w + 1e-37)
+
+
+@pytest.mark.parametrize("dtype,d,decay", [("bf16", 64, 1.0), ("f32", 128, 1.0), ("bf16", 128, 0.9)])
+def test_weights_through_evictions(dtype, d, decay):
+    """Tokens are appended, attend and credit the rows in place; the lightest rows go whenever the cache is full.  Beside it the weights
+    are added up in 64 bits for every row that is kept.  A step's weight is off by at most 2 eps of itself (see test_gpu_cache_weights.py),
+    and each sum by a rounding: the bounds are added up alike.  The choice of the rows is the oracle's from the device's weights."""
+    B, Hkv, G, cap, sink, recent, budget, n, T = 2, 2, 3, 80, 3, 10, 40, 190, DT[dtype]
+    g = torch.Generator().manual_seed(d)
+    K, V = (torch.randn((B, Hkv, n, d), generator=g).to(T).to(DEV) for _ in range(2))
+    q = torch.randn((n, B, Hkv * G, d), generator=g).to(T).to(DEV)
+    caches = [[torch.zeros((B, Hkv, cap, d), dtype=T, device=DEV) for _ in range(2)] + [torch.zeros((B, Hkv, cap), dtype=torch.int32, device=DEV),
+               torch.zeros((B, Hkv, cap), device=DEV)] for _ in range(2)]
+    p = params(B, Hkv * G, Hkv, cap, d, caches[0][0].stride(), T, sink=sink)
+    K64, V64, q64 = (x.double().cpu().numpy() for x in (K, V, q))
+    units = [(b, h) for b in range(B) for h in range(Hkv)]
+    kept = {u: np.zeros(0, np.int64) for u in units}             # tokens whose rows are there, their weights and how far these may be off
+    sums, off = {u: np.zeros(0) for u in units}, {u: np.zeros(0) for u in units}
+    length, evictions = 0, 0
+    for t in range(n):
+        Kc, Vc, pos, acc = caches[0]
+        if length == cap:
+            old = acc.double().cpu().numpy()
+            Ko, Vo, po, ao = caches[1]
+            length = lrsa.lrsa_cache_evict(p, Kc, Vc, pos, acc, length, budget, recent, Ko, Vo, po, ao)
+            for b, h in units:
+                rows = ops.evict_rows(old[b, h], cap, sink, recent, budget)
+                kept[b, h], sums[b, h], off[b, h] = kept[b, h][rows], sums[b, h][rows], off[b, h][rows]
+                assert np.array_equal(po[b, h, :length].cpu().numpy(), kept[b, h]) and bool((ao[b, h, length:] == 0).all())
+            caches.reverse()
+            Kc, Vc, pos, acc = caches[0]
+            evictions += 1
+        Kc[:, :, length], Vc[:, :, length], pos[:, :, length] = K[:, :, t], V[:, :, t], t
+        length += 1
+        lrsa.lrsa_decode_attn_acc(p, q[t], Kc, Vc, length, acc, acc, decay)
+        got = acc.double().cpu().numpy()
+        for b, h in units:
+            rows = kept[b, h] = np.append(kept[b, h], t)
+            qs = q64[t, b, h * G:(h + 1) * G][:, None]
+            _, _, w = ops.attend(qs, K64[b, h, rows], V64[b, h, rows])
+            eps = 2.0 ** -20 * max(8.0, d ** -0.5 * (np.abs(qs[:, 0]) @ np.abs(K64[b, h, rows]).T).max())
+            f = float(np.float32(decay))
+            sums[b, h] = f * np.append(sums[b, h], 0.0) + w
+            off[b, h] = f * np.append(off[b, h], 0.0) + 2 * eps * w + 2.0 ** -23 * sums[b, h]
+            assert np.all(np.abs(got[b, h, :length] - sums[b, h]) <= off[b, h] + 1e-37) and np.all(got[b, h, length:] == 0)
+    assert evictions >= 3 and max((o / s).max() for o, s in zip(off.values(), sums.values())) < 2.0 ** -10
