@@ -319,7 +319,8 @@ int lrsa_cache_evict(const lrsa_params *p, const void *Kc, const void *Vc, const
  * V summed over a cache's rows below 3e38, and int8 codes down to -128.)
  *
  * In these calls p->seq is cap, the rows that the cache has room for; dtype is that of q, O and of the rows K, V given to
- * lrsa_cache_append_quant and taken by lrsa_cache_read_quant, which kv_stride describes; q_stride is not used.  Every sequence
+ * lrsa_cache_append_quant and taken by lrsa_cache_read_quant, which kv_stride describes; what a call does not use (q_stride, lag, topk,
+ * ...) is checked as in every other call.  Every sequence
  * has a length of its own in DEVICE memory, lens [B] int32, so that a captured graph can be replayed while they grow; lengths
  * below 0 count as 0 and lengths above the bound that a call names (max_len, else cap) as that bound. */
 typedef enum { LRSA_QUANT_INT8 = 0, LRSA_QUANT_E4M3 = 1 /* OCP e4m3: no infinities */ } lrsa_quant_format;

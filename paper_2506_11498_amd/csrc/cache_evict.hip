@@ -41,8 +41,9 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
 // lanes and not in 64), then an ordered compaction by ballots.  Integer work only: deterministic.
 // A wave holds 64 * KPT neighbouring rows' keys in registers, four neighbours per lane and group, so the weights are read once; a cache of
 // more than 16 waves' keys is taken in parts, read again in every pass.  One workgroup, because its passes depend on each other; bound by
-// what one CU reads and by some 20 instructions and an LDS atomic per row: 32K rows 16 us, 4.5K rows 5.5 us (keys in LDS instead: 18; an
-// atomic behind a branch per row and pass: 22; keys read again in every pass, as a longer cache does: 43).
+// what one CU reads and by some 20 instructions and an LDS atomic per row: 4.5K rows 7.6 us, 32K rows 16.5 us for 8 heads and 18 to 20 for 32 to
+// 64 (keys in LDS, an atomic behind a branch per row and pass: 1.1 and 1.4 times as long); in parts 32K rows and one 38, 64K 35, 128K 63,
+// more than the move of the rows that stay (8 heads, a quarter of 128K rows of bf16: 51).
 // put(i, r): row r of the old cache becomes row i of the new one.
 template <int KPT, class Put>
 __device__ __forceinline__ void select_rows(const Dims& D, const EvictArgs& E, int unit, int len, Put put) {
@@ -426,9 +427,10 @@ static EvictArgs evict_args(const Dims& D, const int32_t* lens, int len, int bud
 }
 
 // One launch where a workgroup has all keys of its unit in registers and every workgroup a CU of its own, so that the selections that are
-// made several times cost no time.  bf16, d 128, one launch and two: 8 heads, 4501 rows of which 2048 stay 12.4 and 15.5 us, 32 heads (256
-// workgroups) 19.9 and 22.3, 64 heads (256, of 512 rows) 37 and 34, 256 heads, 500 of 1000 rows (256) 34 and 37, 32 heads, 6000 of 8192 rows
-// (384) 53 and 43; 8 bits, 4 heads, 2048 of 8111 rows, and reading them back, 16.4 and 18.7.
+// made several times cost no time.  bf16, d 128, one launch and two: 8 heads, 4501 rows of which 2048 stay 10.4 and 13.0 us, 32 heads (256
+// workgroups) 19.4 and 22.6, 256 heads, 500 of 1000 rows (256) 36 and 39, 64 heads, 4501 rows (256, of 512 rows) 37 and 34, 32 heads, 6000 of 8192
+// rows (384) 56 and 43; 8 bits, 4 heads, 2048 of 8111 rows, 10.1 and 12.6.  With 256 workgroups it is the length of their selections that
+// decides, by 8 % to either side: no rule by length is made of that.
 static bool short_eviction(const Dims& D, int len, int rows, int chunk) {
     return len <= EVICT_SHORT && (int64_t(rows) + chunk - 1) / chunk * D.B * D.Hkv <= 256;
 }

@@ -478,7 +478,7 @@ __global__ __launch_bounds__(DEC_THREADS, 2) void k_decode_quant(Dims D, QuantDi
 }
 
 // Short caches (SHORT_ROWS rows at most, 16 columns): one workgroup per unit, whose 8 waves take all tiles, merge, and write O, lse and
-// the accumulated weights.  A call is one launch, which bounds it (8.4 us, 12 with slices and their merge, call after call: 1 request
+// the accumulated weights.  A call is one launch, which bounds it (8.2 us, 11 with slices and their merge, call after call: 1 request
 // of 777 rows, 12 heads of 64 on 2); but a unit's rows pass through one CU, where slices would spread few units over many.  See
 // short_cache for where that costs more than the launch.
 constexpr int SHORT_WAVES = 8, SHORT_TILES = 4, SHORT_ROWS = SHORT_WAVES * SHORT_TILES * QT;
@@ -657,9 +657,10 @@ hipError_t launch_read_quant(const Dims& D, const QuantDims& Q, const int32_t* l
 }
 
 // Tiles of a slice from which on a wave takes two groups of columns.  Shorter walks are bound by their latency, of which two groups have
-// more.  8 requests on 8 KV heads of 4 query heads, 16 tokens each, bf16, d 128, one group and two: 4K rows (16 tiles) 39.0 and 40.1 us,
-// 8K 60.6 and 56.7, 16K (62) 98.4 and 87.5; 8 tokens: 26.2 and 31.4, 38.8 and 41.8, 61.9 and 58.0; d 64: 18.9 and 21.4, 26.1 and 28.4,
-// 39.7 and 39.5.
+// more.  8 requests on 8 KV heads of 4 query heads, 8 tokens each, bf16, one group and two, us per call: d 128, 4K rows (16 tiles) 35.2 and
+// 37.3, 8K (32) 48.3 and 47.7, 16K (62) 74.3 and 67.7; d 64, 24.0 and 24.8, 33.5 and 32.3, 51.6 and 46.1.  With 16 tokens, where the walk is twice as
+// much work, two groups gain sooner (d 128: 50.9 and 48.6, 78.3 and 69.4, 131 and 112; d 64: 37.2 and 35.8, 56.4 and 50.2, 92.7 and
+// 78.1): the one number is that of few columns.
 constexpr int WIDE_TILES = 40;
 constexpr int64_t PAST_BYTES = int64_t(256) << 20;      // see k_decode_quant
 namespace {
@@ -670,12 +671,12 @@ static QuantPlan quant_plan(const Dims& D, int tokens, int max_len, bool acc) {
     QuantPlan P = {};
     const int64_t units = int64_t(D.B) * D.Hkv;
     // Two workgroups share a CU (registers), so 512 run at once.  With more units than half of that some would have two slices and some
-    // one: then several rounds, of few more slices than units.  8 KV heads, 64 requests of 2048 rows: units + 256 55 us, + 512 58,
-    // + 768 67, + 2048 71; 33 of 4096: 80, 70, 65, 70.
+    // one: then several rounds, of few more slices than units.  8 KV heads, 64 requests of 2048 rows: units + 256 60 us, + 512 63,
+    // + 768 71, + 2048 78; 33 of 4096: 81, 70, 65, 70.
     // With few units of long bf16 rows, one workgroup per CU keeps enough loads in flight, and half as many slices are joined: 8 KV heads, bf16,
     // d 128, 4 columns, 256 and 512 workgroups: 1 request of 16K rows 15.9 us and 17.6, of 128K 50.5 and 54.1, 4 of 40K 59.7 and 62.5, of
-    // 13K to 40K each 50.3 and 51.3, but 8 of 11K to 32K 76.5 and 75.1; 20 columns: 1 of 16K 20.4 and 23.1, of 128K 77.9 and 74.7, 4 of 40K
-    // 90 and 84; d 64, 4 of 40K 39.9 and 37.2; fp32 71 and 64.5.
+    // 13K to 40K each 50.3 and 51.3, but 8 of 11K to 32K 76.5 and 75.1; 20 columns: 1 of 16K 21.5 and 24.1, of 41K 33.0 and 35.5, of 64K 41.5
+    // and 45.0, but of 128K 74 and 71 (taken all the same) and 4 of 40K 84 and 80; d 64, 4 of 40K 39.3 and 34.7; fp32 67 and 65.
     const bool few = D.dtype == 1 && D.d == 128 && units <= (D.G * tokens <= 16 ? 32 : 8);
     const int64_t most = few ? 256 : units <= 256 ? 512 : units + 512;
     const int64_t tiles = (int64_t(max_len) + QT - 1) / QT, fine = units * ((tiles + DEC_WAVES - 1) / DEC_WAVES);
@@ -702,9 +703,9 @@ bool decode_quant_grid_fits(const Dims& D, int tokens, int max_len) {
     return max_len <= 1 << 30 && int64_t(D.B) * ((max_len + QT - 1) / QT) < int64_t(1) << 31 && grid_fits(int64_t(D.B) * D.Hq * tokens + int64_t(D.B) * D.Hkv * ((int64_t(max_len) + DEC_THREADS - 1) / DEC_THREADS), DEC_THREADS);
 }
 
-// One workgroup per unit, or slices?  Heads of 64: one, always (1 request of 1024 rows 8.8 us, slices 12.0; 64 of 1024 16.7, 30.3).
-// Heads of 128 have twice the bytes: one where it is short (12 heads on 2, 100 rows: 8.7, 12.5) or where units fill the card (16 requests
-// of 1000 rows: 13.6, 17.5; 64 of 1024: 32.2, 51.3), slices else (1 request of 1024 rows: 13.8, 12.0).
+// One workgroup per unit, or slices?  Heads of 64: one, always (1 request of 1024 rows 9.1 us, slices 11; 64 of 1024 17.8, 24.1).
+// Heads of 128 have twice the bytes: one where it is short (12 heads on 2, 100 rows: 7.6, 10.3) or where units fill the card (16 requests
+// of 1000 rows: 13.9, 16.1; 64 of 1024: 29.7, 34.2), slices else (1 request of 1024 rows: 13.2, 10.3; 8 of 1024: 13.6, 11.8).
 static bool short_cache(const Dims& D, int cols, int max_len) {
     return cols <= 16 && max_len <= SHORT_ROWS && (D.d == 64 || max_len <= SHORT_ROWS / 2 || int64_t(D.B) * D.Hkv >= 128);
 }
