@@ -1,5 +1,5 @@
 """The inference-cache calls in forms that other tests leave out: 17 to 32 columns over caches larger than the GPU's, weights that are followed through
-evictions.
+evictions, all calls captured without a workspace.
 Oracle and tolerances as in test_gpu_cache_weights.py.
 """
 import numpy as np
@@ -86,3 +86,51 @@ def test_weights_through_evictions(dtype, d, decay):
             off[b, h] = f * np.append(off[b, h], 0.0) + 2 * eps * w + 2.0 ** -23 * sums[b, h]
             assert np.all(np.abs(got[b, h, :length] - sums[b, h]) <= off[b, h] + 1e-37) and np.all(got[b, h, length:] == 0)
     assert evictions >= 3 and max((o / s).max() for o, s in zip(off.values(), sums.values())) < 2.0 ** -10
+
+
+def test_captured_without_a_workspace():
+    """All calls in one graph, outputs and workspaces allocated while it is captured; replayed with other inputs and eager work between."""
+    B, Hkv, G, d, cap, n, T = 2, 2, 4, 128, 2200, 2050, torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(3)
+    K, V, q = (torch.empty(s, dtype=T, device=DEV) for s in ((B, Hkv, cap, d), (B, Hkv, cap, d), (B, Hkv * G, d)))
+    new, lens = [torch.empty((B, Hkv, 1500, d), dtype=T, device=DEV) for _ in range(2)], i32([0, 0])
+    cache, other = (lrsa.QuantCache.empty(B, Hkv, cap, d, torch.int8, 64, DEV) for _ in range(2))
+    Ko, Vo, acc, ao, aq, lo = torch.zeros_like(K), torch.zeros_like(V), *(torch.zeros((B, Hkv, cap), device=DEV) for _ in range(3)), i32([0, 0])
+    p = params(B, Hkv * G, Hkv, cap, d, K.stride(), T, sink=4)
+    pn = params(B, Hkv * G, Hkv, cap, d, new[0].stride(), T, sink=4)
+
+    def calls():
+        O, lse, _ = lrsa.lrsa_decode_attn_acc(p, q, K, V, n, None, acc)
+        lrsa.lrsa_cache_evict(p, K, V, None, acc, n, 700, 50, Ko, Vo, None, ao)
+        lrsa.lrsa_cache_append_quant(pn, cache, *new, lens)
+        end = lens + 1500
+        Oq, lseq = lrsa.lrsa_decode_attn_quant(pn, q, cache, end, cap, None, aq)
+        lrsa.lrsa_cache_evict_quant(pn, cache, None, aq, end, cap, 600, 50, other, None, ao, lo)
+        Kr, Vr = lrsa.lrsa_cache_read_quant(pn, other, lo, 600)
+        return [O, lse, Oq, lseq, Kr, Vr, acc, aq, Ko[:, :, :700], Vo[:, :, :700], lo]
+
+    def fill(k):
+        g.manual_seed(k)
+        for t in (K, V, q, *new):
+            t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+        lens.copy_(i32([k, 600]))
+        for t in (cache.K, cache.V, other.K, other.V, cache.K_scale, cache.V_scale):
+            t.zero_()
+        for t in (acc, aq, Ko, Vo):
+            t.zero_()
+    fill(0)
+    calls()                                                      # everything is loaded before the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    for k in (1, 17, 300):
+        fill(k)
+        want = [t.clone() for t in calls()]
+        fill(k)
+        junk = [torch.empty(1 << 22, device=DEV).normal_() for _ in range(4)]
+        graph.replay()
+        got = [t.clone() for t in out]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), k
+        del junk
