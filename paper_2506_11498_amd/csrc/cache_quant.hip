@@ -710,11 +710,11 @@ static bool short_cache(const Dims& D, int cols, int max_len) {
     return cols <= 16 && max_len <= SHORT_ROWS && (D.d == 64 || max_len <= SHORT_ROWS / 2 || int64_t(D.B) * D.Hkv >= 128);
 }
 
-// Two groups of columns in one wave go past the caches by size like one group (17 to 32 columns; 8 KV heads of 4 query heads, 5 tokens, bf16,
-// us per call on the same cache, through and past the caches: d 128, 83 MB 34 and 37, 163 MB 46 and 52, 229 MB 55 and 61; on others in turn: 33
-// and 37, 48 and 52, 61 and 60; d 64, 86 to 204 MB the same, in turn 35 and 34, 62 and 61), but at any size where weights are accumulated: the
-// logits, 64 bytes or more per row, are then found in the caches when they are read again (d 64, 122 MB, on others in turn 87 and 80, on
-// the same cache 73 and 80; d 128, 229 MB 109 and 99, 96 and 99; 537 MB 249 and 238, 243 and 200).
+// Two groups of columns in one wave (17 to 32 columns): heads of 128 go past the caches by size like one group.  8 KV heads of 4 query heads, 5
+// tokens, bf16, us per call on the same cache, through and past the caches: 83 MB 34 and 37, 163 MB 46 and 52, 229 MB 55 and 61; on others in
+// turn: 33 and 37, 48 and 52, 61 and 60.  At any size heads of 64 do (86 to 204 MB the same, in turn 35 and 34, 43 and 42, 62 and 61), and calls
+// that accumulate weights: the logits, 64 bytes or more per row, are then found in the caches when they are read again (d 64, 122 MB, on
+// others in turn 87 and 80, on the same cache 73 and 80; d 128, 229 MB 109 and 99, 96 and 99; 537 MB 249 and 238, 243 and 200).
 template <typename T, int DH, int FMT>
 static auto decode_quant_kernel(int cols, bool wide, bool past, bool acc) {
     constexpr int MOST = MOST_GROUPS<T, DH>;
@@ -724,7 +724,9 @@ static auto decode_quant_kernel(int cols, bool wide, bool past, bool acc) {
         if (wide) {
             if (cols > 16 * MOST) return acc ? k_decode_quant<T, DH, FMT, MOST, false, false, true> : k_decode_quant<T, DH, FMT, MOST, false, false, false>;
             if (acc) return k_decode_quant<T, DH, FMT, MOST, true, true, true>;
-            return past ? k_decode_quant<T, DH, FMT, MOST, true, true, false> : k_decode_quant<T, DH, FMT, MOST, true, false, false>;
+            if constexpr (DH == 128)
+                if (!past) return k_decode_quant<T, DH, FMT, MOST, true, false, false>;
+            return k_decode_quant<T, DH, FMT, MOST, true, true, false>;
         }
     return acc ? k_decode_quant<T, DH, FMT, 1, false, false, true> : k_decode_quant<T, DH, FMT, 1, false, false, false>;
 }
