@@ -230,7 +230,8 @@ __device__ __forceinline__ void load_quant_tile(QuantTile<DH>& t, const QuantRow
 // NG groups of 16 columns.  seen: rows from the lane's first one on that its column sees; ACC: the logits go to `out`.
 // o is in units of 2^(unit - 127), the power of two of the largest scale of V so far (1 at most, so that no weight gets smaller for it): a weight
 // times a scale of 2^-110 or less has terms below the least bf16 number (2^-133), and would keep 14 bits at 2^-120.  A tile's scales are
-// the same in all lanes (each 16 rows share one), so the unit is a scalar.  It costs 0.2 us in short caches, nothing in long ones.
+// the same in all lanes (each 16 rows share one), so the unit is a scalar.  It costs 0.2 us in short
+// caches, 1 % where the unpacking of codes binds (64 columns over 4 x 40K rows 131.1 and 132.5 us), nothing where memory does.
 constexpr uint32_t LEAST_UNIT = 127 - 120;
 __device__ __forceinline__ float unit_value(uint32_t unit) { return __uint_as_float(unit << 23); }
 template <int DH, int FMT, int TERMS, bool ACC, int NG>
